@@ -346,6 +346,106 @@ mxfp4_status_t mxfp4_change_sums(const void *cur_bf16, const void *prev_bf16, in
 /* The same for two quantized matrices of one shape (the quantized weights of two steps). */
 mxfp4_status_t mxfp4_change_sums_q(mxfp4_mat_t cur, mxfp4_mat_t prev, double *out, void *stream);
 
+/* ---- 8-bit checkpoints of activations ------------------------------------------------------ */
+
+/* What is kept of an activation for the backward pass: E4M3 codes with one power of two for 32 columns, the MX format that is one
+ * step wider than the operands' (1.03 bytes per element).  codes: one byte per element, row pitch cols bytes; scales: one E8M0 byte
+ * (s + 127) per 32 consecutive columns, row major [rows, cols / 32] (these matrices are read by the element-wise passes below, not
+ * by the tensor cores).  cols % 32 == 0.  A group with largest magnitude M has
+ *     s = ceil(log2(M / 448))  (MXFP4_SCALE_TRUNCATION_FREE) or floor(log2 M) - 8  (MXFP4_SCALE_FLOOR),   s >= -127,
+ * M = 0 taking 1e-8 (s = -35), and codes round(v 2^-s) to nearest, ties to even, magnitudes above 448 (floor scaling) to 448.
+ * A group that holds Inf / NaN gets the scale byte 0xFF and codes 0 (MXFP4_DEV_NONFINITE) and reads back as NaN. */
+typedef struct {
+    uint8_t *codes, *scales;   /* codes 16-byte aligned */
+    int64_t rows, cols;
+} mxfp4_ckpt_t;
+
+/* dst = checkpoint of src (bf16 or fp32, dtype MXFP4_OUT_*, [rows, cols], ld elements, rows 16-byte aligned). */
+mxfp4_status_t mxfp4_checkpoint_store(const void *src, int32_t dtype, int64_t ld, mxfp4_ckpt_t dst, int32_t scale_mode, uint32_t *dev_status, void *stream);
+
+/* dst [rows, cols] = what src stands for: exact in fp32; in bf16 exact unless it leaves the normal numbers. */
+mxfp4_status_t mxfp4_checkpoint_load(mxfp4_ckpt_t src, void *dst, int32_t dtype, int64_t ld, void *stream);
+
+/* The activation between two linear layers and the checkpoint of its argument in one pass:
+ *     MXFP4_ACT_GELU (0.5 y (1 + erf(y / sqrt 2))), MXFP4_ACT_SILU (y / (1 + e^-y)):  z = act(y),           y [rows, cols]
+ *     MXFP4_ACT_GEGLU, MXFP4_ACT_SWIGLU:                                              z = act(y_a) * y_b,   y = [y_a, y_b] [rows, 2 cols]
+ * y, z: bf16, rows 16-byte aligned; z is computed in FP32 and rounded once.  ckpt: of y (its cols are y's); codes == NULL: none kept.
+ * z == NULL: not written (the checkpoint alone).  z may lie over y (the same address and leading dimension) unless the activation is
+ * gated; otherwise the outputs must not overlap y. */
+enum { MXFP4_ACT_GELU = 0, MXFP4_ACT_SILU = 1, MXFP4_ACT_GEGLU = 2, MXFP4_ACT_SWIGLU = 3 };
+mxfp4_status_t mxfp4_act_fwd(const void *y_bf16, int64_t ldy, int64_t rows, int64_t cols, int32_t act, void *z_bf16, int64_t ldz, mxfp4_ckpt_t ckpt,
+                             int32_t scale_mode, uint32_t *dev_status, void *stream);
+
+/* Its backward pass from the checkpoint y~:  dy = dz act'(y~), or dy = [dz y~_b act'(y~_a), dz act(y~_a)].  dz bf16 [rows, cols], dy bf16
+ * of ckpt's shape; computed in FP32 and rounded once.  dy may lie over dz (the same address and leading dimension) unless the activation
+ * is gated. */
+mxfp4_status_t mxfp4_act_bwd(const void *dz_bf16, int64_t lddz, mxfp4_ckpt_t ckpt, int32_t act, void *dy_bf16, int64_t lddy, void *stream);
+
+/* ---- residual addition between two norms ---------------------------------------------------- */
+
+/* What stands between two branches of a transformer block, per row of `cols` elements (cols % 32 == 0, cols <= 8192):
+ *     u  = N_post(f)                       the norm behind a branch (kind MXFP4_NORM_NONE: u = f)
+ *     x' = residual_scale * x + branch_scale * g * u
+ *     h  = N_pre(x')                       the norm before the next branch (kind MXFP4_NORM_NONE: no h)
+ * with N(v) = w * v^ + b, v^ = (v - mean v) / sqrt(var v + eps) (MXFP4_NORM_LAYER) or v / sqrt(mean v^2 + eps) (MXFP4_NORM_RMS), w and b
+ * optional (1 and 0).  gate: g is one row of [gates, cols] for each rows / gates consecutive rows (one gate: a layer scale; one
+ * per sequence: what a conditioning projection gives; NULL with gates = 0: 1).
+ * Everything is computed in FP32 (statistics by two passes over the row in registers) and rounded once per output; h and the
+ * checkpoints come from the unrounded x'. */
+enum { MXFP4_NORM_NONE = 0, MXFP4_NORM_LAYER = 1, MXFP4_NORM_RMS = 2 };
+typedef struct {
+    int32_t kind;              /* MXFP4_NORM_* */
+    int32_t dtype;             /* MXFP4_OUT_*: of weight and bias */
+    const void *weight, *bias; /* optional, [cols], 16-byte aligned */
+    float eps;
+    uint32_t reserved;
+} mxfp4_norm_t;
+typedef struct {
+    int64_t rows, cols;
+    int32_t x_dtype;           /* MXFP4_OUT_*: of x, x' and their gradients; f, h and theirs are bf16 */
+    int32_t gate_dtype;        /* MXFP4_OUT_* */
+    float residual_scale, branch_scale;
+    mxfp4_norm_t pre, post;
+    const void *gate;          /* [gates, cols], 16-byte aligned rows, ld_gate elements; rows % gates == 0 */
+    int64_t gates, ld_gate;
+} mxfp4_residual_norm_t;
+
+/* x [rows, cols] and f (optional: x' = x, no x_out; needs post MXFP4_NORM_NONE, no gate and scales of 1) -> x_out and h (either may be
+ * NULL), hq (optional): Q1 of the next linear layer, bit for bit what mxfp4_quantize (round to nearest, scale_mode) makes of h.
+ * For the backward pass: stats (optional) fp32 [4, rows]: mean and 1 / sqrt(var + eps) of N_pre, then of N_post (mean 0 of an RMS norm;
+ * rows of a norm that is absent are left alone); x_ckpt: checkpoint of x^, f_ckpt: of f^ (of f itself without N_post); codes NULL:
+ * not kept.  x_out may lie over x (the same address and leading dimension), h over f likewise. */
+mxfp4_status_t mxfp4_residual_norm_fwd(const mxfp4_residual_norm_t *n, const void *x, int64_t ldx, const void *f_bf16, int64_t ldf, void *x_out, int64_t ldxo,
+                                       void *h_bf16, int64_t ldh, const mxfp4_mat_t *hq, float *stats, mxfp4_ckpt_t x_ckpt, mxfp4_ckpt_t f_ckpt,
+                                       int32_t scale_mode, uint32_t *dev_status, void *stream);
+
+/* The gradients of what the struct describes.  dh (NULL without N_pre) and dx_out (gradient of x' from further on; NULL: 0) come in.
+ * Of the forward pass: stats, and x^ and f^ either as checkpoints (codes != NULL) or as x_out and f themselves (both or neither of
+ * the two in 8 bits; x_out is read where there is N_pre, f where there is N_post or a gate).
+ * Out, all optional but dx: dx (x_dtype), df (bf16; NULL also means that there was no f), and in FP32, written whole: dw_pre, db_pre, dw_post, db_post
+ * [cols], dgate [gates, cols].  Sums over rows are taken in FP32 in an order that depends on the shape and the number of SMs alone: the same
+ * call gives the same bits.  dx may lie over dx_out (the same address and leading dimension), df over dh likewise.
+ * workspace: >= mxfp4_residual_norm_workspace_bytes, 256-byte aligned; its contents do not matter. */
+size_t mxfp4_residual_norm_workspace_bytes(int64_t rows, int64_t cols, int64_t gates);
+typedef struct {
+    const void *dh_bf16;
+    int64_t lddh;
+    const void *dx_out;
+    int64_t lddxo;
+    const float *stats;
+    mxfp4_ckpt_t x_ckpt, f_ckpt;
+    const void *x_out;
+    int64_t ldxo;
+    const void *f_bf16;
+    int64_t ldf;
+    void *dx;
+    int64_t lddx;
+    void *df_bf16;
+    int64_t lddf;
+    float *dw_pre, *db_pre, *dw_post, *db_post, *dgate;
+} mxfp4_residual_norm_bwd_t;
+mxfp4_status_t mxfp4_residual_norm_bwd(const mxfp4_residual_norm_t *n, const mxfp4_residual_norm_bwd_t *b, void *workspace, size_t workspace_bytes, void *stream);
+
 /* ---- quantized linear layer (Sec. 3.3) ----------------------------------------------------- */
 
 /* Forward, Eq. 3: Y = Q1(X) Q2(W)^T.  x bf16 [M, K] (ldx), y bf16 [M, N] (ldy).

@@ -4,4 +4,6 @@ from .binding import (  # noqa: F401
     SCALE_FLOOR, SCALE_TRUNCATION_FREE, STATIC_SCRATCH_BYTES, LinearCtx, MxError, OscState, QMat, dequantize, gemm, gemm_static,
     gemm_chain_mmas, gemm_wait_selftest, forward_wait_selftest, launch_count, gemm_workspace_bytes, quantize_wait_selftest, lib, linear_bwd, linear_fwd, linear_workspace_bytes, new_status, qema_quantize, qramp_adamw, qramp_detect, quant_conf_hist, change_sums, mma_issue_ceiling,
     quantize, quantize_2axis, quantize_chain, quantize_t, scale_bytes, scale_offset,
+    ACT_GEGLU, ACT_GELU, ACT_SILU, ACT_SWIGLU, NORM_LAYER, NORM_RMS, SAVE_8BIT, SAVE_INPUTS, SAVE_NOTHING, Checkpoint, Norm, NormCtx, NormGrads, act_bwd, act_fwd,
+    checkpoint_load, checkpoint_store, residual_norm_bwd, residual_norm_fwd, residual_norm_workspace_bytes,
 )

@@ -7,6 +7,7 @@ torch is used for device memory and streams.  The library and the module must be
 import copyreg
 import ctypes as C
 import os
+from collections import namedtuple
 
 import torch
 
@@ -35,6 +36,9 @@ ROUND_NEAREST, ROUND_STOCHASTIC = 0, 1
 OUT_BF16, OUT_FP32 = 0, 1
 DEV_NONFINITE, DEV_TIMEOUT, DEV_SMEM_LAYOUT = 1, 2, 4
 HOOK_IDENTITY, HOOK_GELU, HOOK_MULTIPLY = 0, 1, 2
+ACT_GELU, ACT_SILU, ACT_GEGLU, ACT_SWIGLU = 0, 1, 2, 3
+NORM_LAYER, NORM_RMS = 1, 2
+SAVE_NOTHING, SAVE_8BIT, SAVE_INPUTS = 0, 1, 2
 
 STATUS_NAMES = {0: "OK", 1: "INVALID_ARG", 2: "BAD_SHAPE", 3: "MISALIGNED", 4: "WORKSPACE_TOO_SMALL",
                 5: "UNSUPPORTED_DEVICE", 6: "CUDA_ERROR"}
@@ -44,7 +48,8 @@ EXPORTS = ["mxfp4_launch_count", "mxfp4_scale_bytes", "mxfp4_scale_offset", "mxf
            "mxfp4_qema_quantize", "mxfp4_dequantize", "mxfp4_gemm", "mxfp4_gemm_quant", "mxfp4_gemm_static", "mxfp4_linear_fwd",
            "mxfp4_linear_bwd", "mxfp4_linear_fwd_ex", "mxfp4_linear_bwd_ex", "mxfp4_qramp_adamw", "mxfp4_qramp_detect", "mxfp4_quant_conf_hist", "mxfp4_change_sums",
            "mxfp4_change_sums_q", "mxfp4_mma_issue_ceiling", "mxfp4_gemm_wait_selftest", "mxfp4_quantize_wait_selftest",
-           "mxfp4_forward_wait_selftest"]
+           "mxfp4_forward_wait_selftest", "mxfp4_checkpoint_store", "mxfp4_checkpoint_load", "mxfp4_act_fwd", "mxfp4_act_bwd",
+           "mxfp4_residual_norm_fwd", "mxfp4_residual_norm_bwd", "mxfp4_residual_norm_workspace_bytes"]
 
 
 class MxError(RuntimeError):
@@ -83,6 +88,28 @@ class CEpilogue(C.Structure):
 class CCtx(C.Structure):
     _fields_ = [("xq", CMat), ("wq", CMat), ("xq_t", CMat), ("xq_t_seed", C.c_uint64), ("wq_t", CMat), ("wq_t_seed", C.c_uint64)]
 
+
+class CCkpt(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("rows", C.c_int64), ("cols", C.c_int64)]
+
+
+class CNorm(C.Structure):
+    _fields_ = [("kind", C.c_int32), ("dtype", C.c_int32), ("weight", C.c_void_p), ("bias", C.c_void_p), ("eps", C.c_float), ("reserved", C.c_uint32)]
+
+
+class CResidualNorm(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("cols", C.c_int64), ("x_dtype", C.c_int32), ("gate_dtype", C.c_int32), ("residual_scale", C.c_float),
+                ("branch_scale", C.c_float), ("pre", CNorm), ("post", CNorm), ("gate", C.c_void_p), ("gates", C.c_int64), ("ld_gate", C.c_int64)]
+
+
+class CResidualNormBwd(C.Structure):
+    _fields_ = [("dh", C.c_void_p), ("lddh", C.c_int64), ("dx_out", C.c_void_p), ("lddxo", C.c_int64), ("stats", C.c_void_p), ("x_ckpt", CCkpt),
+                ("f_ckpt", CCkpt), ("x_out", C.c_void_p), ("ldxo", C.c_int64), ("f", C.c_void_p), ("ldf", C.c_int64), ("dx", C.c_void_p), ("lddx", C.c_int64),
+                ("df", C.c_void_p), ("lddf", C.c_int64), ("dw_pre", C.c_void_p), ("db_pre", C.c_void_p), ("dw_post", C.c_void_p), ("db_post", C.c_void_p),
+                ("dgate", C.c_void_p)]
+
+
+_NO_CKPT, _NO_NORM = CCkpt(None, None, 0, 0), CNorm(0, 0, None, None, 0.0, 0)
 
 _lib = None
 
@@ -166,6 +193,20 @@ def lib():
     L.mxfp4_qramp_detect.argtypes = [vp, vp, i64, C.c_float, i32, i32, vp, vp, vp]
     L.mxfp4_qramp_adamw.restype = i32
     L.mxfp4_qramp_adamw.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, i64, C.POINTER(CAdamW), vp]
+    L.mxfp4_checkpoint_store.restype = i32
+    L.mxfp4_checkpoint_store.argtypes = [vp, i32, i64, CCkpt, i32, vp, vp]
+    L.mxfp4_checkpoint_load.restype = i32
+    L.mxfp4_checkpoint_load.argtypes = [CCkpt, vp, i32, i64, vp]
+    L.mxfp4_act_fwd.restype = i32
+    L.mxfp4_act_fwd.argtypes = [vp, i64, i64, i64, i32, vp, i64, CCkpt, i32, vp, vp]
+    L.mxfp4_act_bwd.restype = i32
+    L.mxfp4_act_bwd.argtypes = [vp, i64, CCkpt, i32, vp, i64, vp]
+    L.mxfp4_residual_norm_fwd.restype = i32
+    L.mxfp4_residual_norm_fwd.argtypes = [C.POINTER(CResidualNorm), vp, i64, vp, i64, vp, i64, vp, i64, C.POINTER(CMat), vp, CCkpt, CCkpt, i32, vp, vp]
+    L.mxfp4_residual_norm_bwd.restype = i32
+    L.mxfp4_residual_norm_bwd.argtypes = [C.POINTER(CResidualNorm), C.POINTER(CResidualNormBwd), vp, sz, vp]
+    L.mxfp4_residual_norm_workspace_bytes.restype = sz
+    L.mxfp4_residual_norm_workspace_bytes.argtypes = [i64, i64, i64]
     # the entry points that _host calls
     for name in ("linear_fwd_ex", "linear_bwd_ex", "quantize", "quantize_t", "qema_quantize"):
         setattr(L, "at_" + name, C.cast(getattr(L, "mxfp4_" + name), C.c_void_p).value)
@@ -185,6 +226,7 @@ try:
     def _stream():
         return _raw_stream(_device())
 except AttributeError:      # they are internal to torch
+    _device = torch.cuda.current_device
 
     def _stream():
         return torch.cuda.current_stream().cuda_stream
@@ -640,6 +682,226 @@ def change_sums(cur, prev, out=None):
         assert cur.shape == prev.shape
         _check("mxfp4_change_sums", lib().mxfp4_change_sums(_ptr(cur), _ptr(prev), cur.numel(), _ptr(res), _stream()))
     return res
+
+
+# ---- 8-bit checkpoints of activations ----
+
+_OUT_OF = {torch.bfloat16: OUT_BF16, torch.float32: OUT_FP32}
+_DTYPES = (torch.bfloat16, torch.float32)
+
+
+def _rows(x, shape=None, dtype=None):
+    """A row-major matrix on the current device, of bf16 or fp32 (or of ``dtype``) and, where that is given, of ``shape``."""
+    assert x.is_cuda and x.get_device() == _device() and x.dtype in _DTYPES and x.dim() == 2 and x.stride(1) == 1
+    assert (dtype is None or x.dtype == dtype) and (shape is None or x.shape == shape), "another type or shape is expected"
+    return x
+
+
+def _here(t, dtype, shape):
+    """A contiguous tensor on the current device."""
+    assert t is None or (t.is_cuda and t.get_device() == _device() and t.dtype == dtype and t.shape == shape and t.is_contiguous())
+    return t
+
+
+class Checkpoint:
+    """An activation kept in 8 bits: E4M3 ``codes`` (uint8 [rows, cols]) and one E8M0 byte per 32 columns, ``scales`` (uint8 [rows, cols / 32])."""
+
+    __slots__ = ("codes", "scales")
+
+    def __init__(self, codes, scales):
+        assert codes.dtype == torch.uint8 and scales.dtype == torch.uint8 and codes.dim() == 2 and codes.is_contiguous() and scales.is_contiguous()
+        assert codes.shape[1] % 32 == 0 and tuple(scales.shape) == (codes.shape[0], codes.shape[1] // 32) and codes.device == scales.device
+        self.codes, self.scales = codes, scales
+
+    @staticmethod
+    def empty(rows, cols, device="cuda"):
+        assert cols % 32 == 0
+        return Checkpoint(_new((rows, cols), torch.uint8, device), _new((rows, cols // 32), torch.uint8, device))
+
+    @property
+    def shape(self):
+        return self.codes.shape
+
+    @property
+    def device(self):
+        return self.codes.device
+
+    def c(self):
+        return CCkpt(self.codes.data_ptr(), self.scales.data_ptr(), self.codes.shape[0], self.codes.shape[1])
+
+
+def _ckpt(c, shape=None):
+    if c is None:
+        return _NO_CKPT
+    assert c.codes.is_cuda and c.codes.get_device() == _device() and (shape is None or c.codes.shape == shape)
+    return c.c()
+
+
+def checkpoint_store(x, scale_mode=SCALE_TRUNCATION_FREE, out=None, dev_status=None):
+    """The 8-bit checkpoint of x (bf16 or fp32 [rows, cols], cols a multiple of 32)."""
+    x = _rows(x)
+    out = out if out is not None else Checkpoint.empty(*x.shape, x.device)
+    _check("mxfp4_checkpoint_store", lib().mxfp4_checkpoint_store(x.data_ptr(), _OUT_OF[x.dtype], x.stride(0), _ckpt(out, x.shape), scale_mode, _ptr(dev_status), _stream()))
+    return out
+
+
+def checkpoint_load(ckpt, out_dtype=OUT_BF16, out=None):
+    """What a checkpoint stands for, as bf16 or fp32."""
+    if out is None:
+        out = _new(tuple(ckpt.shape), _DTYPES[out_dtype], ckpt.device)
+    out = _rows(out, ckpt.shape)
+    _check("mxfp4_checkpoint_load", lib().mxfp4_checkpoint_load(_ckpt(ckpt), out.data_ptr(), _OUT_OF[out.dtype], out.stride(0), _stream()))
+    return out
+
+
+def _halves(act):
+    return 2 if act in (ACT_GEGLU, ACT_SWIGLU) else 1
+
+
+def act_fwd(y, act=ACT_GELU, save=SAVE_8BIT, scale_mode=SCALE_TRUNCATION_FREE, out=None, ckpt=None, dev_status=None):
+    """z = act(y), or act(y_a) y_b for the gated activations on y = [y_a, y_b], and the 8-bit checkpoint of y that act_bwd reads
+    (``save=SAVE_NOTHING``: None).  y: bf16 [rows, cols] (gated: [rows, 2 cols])."""
+    y = _rows(y, dtype=torch.bfloat16)
+    assert save in (SAVE_NOTHING, SAVE_8BIT) and y.shape[1] % _halves(act) == 0
+    rows, cols = y.shape[0], y.shape[1] // _halves(act)
+    out = _rows(out if out is not None else _new((rows, cols), torch.bfloat16, y.device), (rows, cols), torch.bfloat16)
+    if ckpt is None and save == SAVE_8BIT:
+        ckpt = Checkpoint.empty(*y.shape, y.device)
+    _check("mxfp4_act_fwd", lib().mxfp4_act_fwd(y.data_ptr(), y.stride(0), rows, cols, act, out.data_ptr(), out.stride(0), _ckpt(ckpt, y.shape), scale_mode,
+                                                _ptr(dev_status), _stream()))
+    return out, ckpt
+
+
+def act_bwd(dz, ckpt, act=ACT_GELU, out=None):
+    """The gradient of y from that of z and the checkpoint of y."""
+    rows, ycols = ckpt.shape
+    dz = _rows(dz, (rows, ycols // _halves(act)), torch.bfloat16)
+    out = _rows(out if out is not None else _new((rows, ycols), torch.bfloat16, dz.device), (rows, ycols), torch.bfloat16)
+    _check("mxfp4_act_bwd", lib().mxfp4_act_bwd(dz.data_ptr(), dz.stride(0), _ckpt(ckpt), act, out.data_ptr(), out.stride(0), _stream()))
+    return out
+
+
+# ---- residual addition between two norms ----
+
+class Norm:
+    """A norm over the columns: NORM_LAYER or NORM_RMS, weight and bias ([cols], one type, bf16 or fp32; either may be None: 1 and 0)."""
+
+    __slots__ = ("kind", "weight", "bias", "eps")
+
+    def __init__(self, kind=NORM_LAYER, weight=None, bias=None, eps=1e-6):
+        self.kind, self.weight, self.bias, self.eps = kind, weight, bias, eps
+
+    def c(self, cols):
+        w, b = self.weight, self.bias
+        one = w if w is not None else b
+        if one is None:
+            return CNorm(self.kind, 0, None, None, self.eps, 0)
+        for t in (w, b):    # of one type
+            _here(t, one.dtype, (cols,))
+        return CNorm(self.kind, _OUT_OF[one.dtype], _ptr(w), _ptr(b), self.eps, 0)
+
+
+class NormCtx:
+    """What residual_norm_fwd leaves for residual_norm_bwd: the plan (norms, gate, scales), the rows' statistics, and x^ and f^ as Checkpoints
+    or x_out and f themselves (None where the backward pass reads none)."""
+
+    __slots__ = ("x", "f", "stats", "pre", "post", "gate", "residual_scale", "branch_scale")
+
+    def __init__(self, x, f, stats, pre=None, post=None, gate=None, residual_scale=1.0, branch_scale=1.0):
+        self.x, self.f, self.stats, self.pre, self.post, self.gate = x, f, stats, pre, post, gate
+        self.residual_scale, self.branch_scale = residual_scale, branch_scale
+
+
+NormGrads = namedtuple("NormGrads", "dx df pre_weight pre_bias post_weight post_bias gate")
+
+
+def _residual_norm(rows, cols, x_dtype, pre, post, gate, residual_scale, branch_scale):
+    gates = ld = gd = 0
+    if gate is not None:
+        gate = _rows(gate if gate.dim() == 2 else gate.view(1, -1))
+        assert gate.shape[1] == cols
+        gates, ld, gd = gate.shape[0], gate.stride(0), _OUT_OF[gate.dtype]
+    return CResidualNorm(rows, cols, _OUT_OF[x_dtype], gd, residual_scale, branch_scale, pre.c(cols) if pre is not None else _NO_NORM,
+                         post.c(cols) if post is not None else _NO_NORM, _ptr(gate), gates, ld)
+
+
+def residual_norm_fwd(x, f=None, pre=None, post=None, gate=None, residual_scale=1.0, branch_scale=1.0, save=SAVE_8BIT, x_out=None, h=None, hq=None,
+                      scale_mode=SCALE_TRUNCATION_FREE, dev_status=None):
+    """The end of one branch of a transformer block and the start of the next, in one pass:
+        x_out = residual_scale * x + branch_scale * gate * post(f),   h = pre(x_out).
+    x: bf16 or fp32 [rows, cols]; f: bf16, the branch's result (None: h = pre(x) alone); pre, post: Norm or None; gate: [cols] or [gates, cols], a row
+    for each rows / gates consecutive rows.  ``hq``: a QMat to fill with Q1(h), the next linear layer's operand (``h=False`` then leaves h itself out).
+    ``save``: what the backward pass will read: the normalized rows in 8 bits, the inputs themselves (x_out and f, which must then stay as they
+    are), or nothing.  Returns (x_out, h, NormCtx or None)."""
+    x = _rows(x)
+    shape = rows, cols = x.shape
+    if f is not None:
+        f = _rows(f, shape, torch.bfloat16)
+        x_out = _rows(x_out if x_out is not None else _new(shape, x.dtype, x.device), shape, x.dtype)
+    else:
+        assert x_out is None
+    if h is False or pre is None:
+        assert h is None or h is False
+        h = None
+    else:
+        h = _rows(h if h is not None else _new(shape, torch.bfloat16, x.device), shape, torch.bfloat16)
+    plan = _residual_norm(rows, cols, x.dtype, pre, post, gate, residual_scale, branch_scale)
+    kx = kf = stats = ctx = None
+    if save != SAVE_NOTHING:
+        assert save in (SAVE_8BIT, SAVE_INPUTS)
+        keep_f = f is not None and (post is not None or gate is not None)
+        if pre is not None or post is not None:
+            stats = _new((4, rows), torch.float32, x.device)
+        if save == SAVE_8BIT:
+            kx = Checkpoint.empty(rows, cols, x.device) if pre is not None else None
+            kf = Checkpoint.empty(rows, cols, x.device) if keep_f else None
+            ctx = NormCtx(kx, kf, stats, pre, post, gate, residual_scale, branch_scale)
+        else:
+            ctx = NormCtx((x_out if f is not None else x) if pre is not None else None, f if keep_f else None, stats, pre, post, gate, residual_scale, branch_scale)
+    cq = hq.c() if hq is not None else None
+    _check("mxfp4_residual_norm_fwd",
+           lib().mxfp4_residual_norm_fwd(C.byref(plan), x.data_ptr(), x.stride(0), _ptr(f), f.stride(0) if f is not None else 0, _ptr(x_out),
+                                         x_out.stride(0) if x_out is not None else 0, _ptr(h), h.stride(0) if h is not None else 0,
+                                         C.byref(cq) if cq is not None else None, _ptr(stats), _ckpt(kx), _ckpt(kf), scale_mode, _ptr(dev_status), _stream()))
+    return x_out, h, ctx
+
+
+def residual_norm_workspace_bytes(rows, cols, gates):
+    return int(lib().mxfp4_residual_norm_workspace_bytes(rows, cols, gates))
+
+
+def residual_norm_bwd(dh, dx_out, ctx, dx=None, df=None, workspace=None):
+    """The gradients of residual_norm_fwd: NormGrads(dx, df, and in fp32 those of the norms' weights and biases [cols] and of the gate [gates, cols];
+    None where there is no such thing).  dh: bf16, the gradient of h (None without ``pre``); dx_out: that of x_out from further on, in x's
+    type (None: 0).  ``df=False``: leaves it out (there was no f)."""
+    pre, post, gate = ctx.pre, ctx.post, ctx.gate
+    eight = isinstance(ctx.x if ctx.x is not None else ctx.f, Checkpoint)
+    given = dx_out if dx_out is not None else dh
+    shape = rows, cols = given.shape
+    dev = given.device
+    x_dtype = dx_out.dtype if dx_out is not None else dx.dtype if dx is not None else ctx.x.dtype if not eight and ctx.x is not None else torch.bfloat16
+    if dh is not None:
+        dh = _rows(dh, shape, torch.bfloat16)
+    if dx_out is not None:
+        dx_out = _rows(dx_out, shape)
+    x, f = ctx.x, ctx.f
+    if not eight:
+        x, f = x if x is None else _rows(x, shape, x_dtype), f if f is None else _rows(f, shape, torch.bfloat16)
+    dx = _rows(dx if dx is not None else _new(shape, x_dtype, dev), shape, x_dtype)
+    df = None if df is False else _rows(df if df is not None else _new(shape, torch.bfloat16, dev), shape, torch.bfloat16)
+    plan = _residual_norm(rows, cols, x_dtype, pre, post, gate, ctx.residual_scale, ctx.branch_scale)
+    new = lambda yes, n=1: _new((n, cols) if n > 1 else (cols,), torch.float32, dev) if yes else None  # noqa: E731
+    gw, gb = new(pre is not None and pre.weight is not None), new(pre is not None and pre.bias is not None)
+    qw, qb = new(post is not None and post.weight is not None), new(post is not None and post.bias is not None)
+    gg = _new((max(plan.gates, 1), cols), torch.float32, dev) if gate is not None else None
+    if workspace is None:
+        workspace = _new((max(residual_norm_workspace_bytes(rows, cols, plan.gates), 256),), torch.uint8, dev)
+    b = CResidualNormBwd(_ptr(dh), dh.stride(0) if dh is not None else 0, _ptr(dx_out), dx_out.stride(0) if dx_out is not None else 0,
+                         _ptr(_here(ctx.stats, torch.float32, (4, rows))), *((_ckpt(x, shape), _ckpt(f, shape), None, 0, None, 0) if eight else
+                         (_NO_CKPT, _NO_CKPT, _ptr(x), x.stride(0) if x is not None else 0, _ptr(f), f.stride(0) if f is not None else 0)), dx.data_ptr(), dx.stride(0), _ptr(df),
+                         df.stride(0) if df is not None else 0, _ptr(gw), _ptr(gb), _ptr(qw), _ptr(qb), _ptr(gg))
+    _check("mxfp4_residual_norm_bwd", lib().mxfp4_residual_norm_bwd(C.byref(plan), C.byref(b), workspace.data_ptr(), workspace.numel(), _stream()))
+    return NormGrads(dx, df, gw, gb, qw, qb, gg)
 
 
 def mma_issue_ceiling(bn=256, iters=2000, reps=5):

@@ -134,14 +134,8 @@ __device__ __forceinline__ uint64_t fma_f32x2(uint64_t a, uint64_t b, float c)
 // and gives zero from y = -5.6 on.  Product and quantizer at 25216 x 1536 x 384: 58.5 us with that, 60.0 with this, 61.6 with
 // degree 12 (6.6e-8 |y|, 17 results).
 // +Inf gives +Inf (its magnitude is cut to the largest finite one: e = 0), -Inf and NaN give NaN.
-__device__ __forceinline__ uint32_t gelu_bf16x2(uint32_t w)
+__device__ __forceinline__ uint64_t gelu_tail_log2(uint64_t a)   // of a pair |y| / 8: log2(8 e)
 {
-    uint32_t cut, pos;
-    asm("min.NaN.bf16x2 %0, %1, %2;" : "=r"(cut) : "r"(w), "r"(0x7F7F7F7Fu));
-    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(pos) : "r"(w), "r"(0x80008000u));   // -0 for y <= -0: a zero keeps its sign
-    float a0, a1, p0, p1, e0, e1, t0, t1;
-    scale_pair(cut & 0x7FFF7FFFu, 0x3E003E00u, a0, a1);
-    const uint64_t a = f32x2(a0, a1);
     uint64_t p = fma_f32x2(f32x2(-2.7756042e+00f, -2.7756042e+00f), a, 1.7597485e+01f);
     p = fma_f32x2(p, a, -4.435496e+01f);
     p = fma_f32x2(p, a, 5.4649006e+01f);
@@ -151,7 +145,17 @@ __device__ __forceinline__ uint32_t gelu_bf16x2(uint32_t w)
     p = fma_f32x2(p, a, -2.696964e+01f);
     p = fma_f32x2(p, a, -2.9386005e+01f);
     p = fma_f32x2(p, a, -9.208879e+00f);
-    p = fma_f32x2(p, a, 2.0f);
+    return fma_f32x2(p, a, 2.0f);
+}
+__device__ __forceinline__ uint32_t gelu_bf16x2(uint32_t w)
+{
+    uint32_t cut, pos;
+    asm("min.NaN.bf16x2 %0, %1, %2;" : "=r"(cut) : "r"(w), "r"(0x7F7F7F7Fu));
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(pos) : "r"(w), "r"(0x80008000u));   // -0 for y <= -0: a zero keeps its sign
+    float a0, a1, p0, p1, e0, e1, t0, t1;
+    scale_pair(cut & 0x7FFF7FFFu, 0x3E003E00u, a0, a1);
+    const uint64_t a = f32x2(a0, a1);
+    const uint64_t p = gelu_tail_log2(a);
     asm("mov.b64 {%0, %1}, %2;" : "=f"(p0), "=f"(p1) : "l"(p));
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e0) : "f"(p0));
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e1) : "f"(p1));
