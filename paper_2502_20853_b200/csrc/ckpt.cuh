@@ -127,10 +127,14 @@ __device__ __forceinline__ void e4m3_to8(const uint2 &c, float scale, f2 (&o)[4]
 // Largest magnitude of a lane's eight values as a bit pattern (what is not finite compares as larger than everything finite).
 __device__ __forceinline__ uint32_t amax8(const f2 (&v)[4])
 {
-    uint32_t m = 0;
+    float a[8], m;
 #pragma unroll
-    for (int j = 0; j < 4; j++) m = max(m, max((uint32_t)v[j] & 0x7FFFFFFFu, (uint32_t)(v[j] >> 32) & 0x7FFFFFFFu));
-    return m;
+    for (int j = 0; j < 4; j++) f2_to(v[j], a[2 * j], a[2 * j + 1]);
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(m) : "f"(a[0]), "f"(a[1]), "f"(a[2]));       // a NaN gives 0x7FFFFFFF
+    asm("max.NaN.abs.f32 %0, %0, %1, %2;" : "+f"(m) : "f"(a[3]), "f"(a[4]));
+    asm("max.NaN.abs.f32 %0, %0, %1, %2;" : "+f"(m) : "f"(a[5]), "f"(a[6]));
+    asm("max.NaN.abs.f32 %0, %0, %1, %1;" : "+f"(m) : "f"(a[7]));
+    return __float_as_uint(m);
 }
 // ... and of its group of four lanes.  All lanes of the warp take part.
 __device__ __forceinline__ uint32_t group_max4(uint32_t m)

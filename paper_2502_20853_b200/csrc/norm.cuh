@@ -1,0 +1,223 @@
+// What the two directions of the residual addition between norms share: teams, the ring of rows, parameters, the host's plan.
+//
+// A team of T lanes (a power of two from 4 to 256) holds a row in registers, each lane V vectors of eight columns: vector v * T + t.
+// The sums over a row go through shuffles and, where a team has several warps, through shared memory and a barrier of the team.
+// V is 3 or 4: with T a power of two these two reach every width within a third, and the usual widths (384 = 8 x 16 x 3, 768, 1024)
+// exactly; long lanes keep the shuffles few (five for 768 or 1024 columns).
+// One block of eight warps per SM; each team takes a run of consecutive rows, so that its lanes keep their columns: what belongs to a
+// column (weights, gates, sums over rows) stays in registers from row to row.  Eight warps cannot hide the memory's latency by
+// themselves; a lane's share of the next rows travels into shared memory meanwhile (cp.async into slots that only this lane reads: no
+// barriers).
+// FULL: T V vectors are exactly a row.  The kernels are bound by the instructions they issue, and without the masks of a partly filled
+// lane the loops over V are straight code.
+#pragma once
+#include "ckpt.cuh"
+#include "quant_tile.cuh"
+#include "tma.cuh"
+
+namespace mx {
+
+constexpr int kNormMaxCols = 8192;
+constexpr int kThreads = 256;
+
+// ---- a lane's ring of rows in shared memory ----------------------------------------------------
+__device__ __forceinline__ void async16(uint32_t dst, const void *src) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory"); }
+__device__ __forceinline__ void async8(uint32_t dst, const void *src) { asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory"); }
+__device__ __forceinline__ void async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT> __device__ __forceinline__ void async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
+__device__ __forceinline__ uint4 lds16(uint32_t at)
+{
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
+    return v;
+}
+__device__ __forceinline__ uint2 lds8(uint32_t at)
+{
+    uint2 v;
+    asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at));
+    return v;
+}
+// Eight elements of type T: slots of 16 bytes per lane, one (bf16) or two (fp32) of them.  A block's lanes lie side by side.
+template <class T> constexpr int kSlots = sizeof(T) / 2;
+template <class T> __device__ __forceinline__ void async_row8(uint32_t slot, const T *src)
+{
+    async16(slot, src);
+    if (sizeof(T) == 4) async16(slot + kThreads * 16, src + 4);
+}
+template <class T> __device__ __forceinline__ void ring_row8(uint32_t slot, f2 (&o)[4])
+{
+    const uint4 a = lds16(slot);
+    if (sizeof(T) == 2) {
+        unpack8(a, o);
+    } else {
+        const uint4 b = lds16(slot + kThreads * 16);
+        o[0] = (f2)a.y << 32 | a.x, o[1] = (f2)a.w << 32 | a.z, o[2] = (f2)b.y << 32 | b.x, o[3] = (f2)b.w << 32 | b.z;
+    }
+}
+// As many stages as fit beside `other` bytes, four at most.
+constexpr int ring_depth(int stage, int other) { return (220 * 1024 - other) / stage < 4 ? (220 * 1024 - other) / stage : 4; }
+__device__ __forceinline__ void zero8(f2 (&o)[4]) { o[0] = o[1] = o[2] = o[3] = 0; }
+
+// ---- teams --------------------------------------------------------------------------------------
+struct Team {
+    int lanes, lane;     // of the team
+    int id;              // of the team in its block
+    float4 *slots;       // several warps: where they leave their sums, two sets that take turns
+    int turn;
+};
+
+// Rows of which a team of several in a warp has none left take part in its shuffles; `turns` is the same for all teams of a warp.
+__device__ __forceinline__ int64_t turns_of(const Team &t, int64_t rows_per_team, int64_t first, int64_t end) { return t.lanes < 32 ? rows_per_team : end - first; }
+
+__device__ __forceinline__ Team make_team(int log2_lanes, float4 *smem)
+{
+    Team t;
+    t.lanes = 1 << log2_lanes;
+    t.lane = threadIdx.x & (t.lanes - 1);
+    t.id = threadIdx.x >> log2_lanes;
+    t.slots = smem + t.id * 2 * (t.lanes >> 5);
+    t.turn = 0;
+    return t;
+}
+
+// The sums of N (1, 2) numbers over the lanes of the team, the same bits in each of them.  All lanes of the warp take part.
+template <int N>
+__device__ __forceinline__ void team_sum(Team &t, float (&v)[N])
+{
+    const int in_warp = min(t.lanes, 32);
+    for (int o = in_warp >> 1; o; o >>= 1)
+#pragma unroll
+        for (int k = 0; k < N; k++) v[k] += __shfl_xor_sync(0xFFFFFFFFu, v[k], o);
+    if (t.lanes > 32) {
+        const int warps = t.lanes >> 5;
+        float *s = reinterpret_cast<float *>(t.slots + t.turn * warps);
+        t.turn ^= 1;     // a warp that is ahead writes the other set: nobody is more than one barrier ahead
+        if ((t.lane & 31) == 0)
+#pragma unroll
+            for (int k = 0; k < N; k++) s[(t.lane >> 5) * 4 + k] = v[k];
+        asm volatile("bar.sync %0, %1;" ::"r"(t.id + 1), "r"(t.lanes) : "memory");
+#pragma unroll
+        for (int k = 0; k < N; k++) v[k] = 0.0f;
+        for (int w = 0; w < warps; w++)
+#pragma unroll
+            for (int k = 0; k < N; k++) v[k] += s[w * 4 + k];
+    }
+}
+
+// ---- parameters ---------------------------------------------------------------------------------
+struct NormSide {
+    const void *w, *b;   // either may be missing
+    int fp32;
+    int rms;
+    float eps;
+};
+__device__ __forceinline__ void load_param8(const void *p, int fp32, int64_t at, f2 (&o)[4])
+{
+    if (fp32) {
+        const uint4 *q = reinterpret_cast<const uint4 *>(static_cast<const float *>(p) + at);
+        const uint4 a = q[0], b = q[1];
+        o[0] = (f2)a.y << 32 | a.x, o[1] = (f2)a.w << 32 | a.z, o[2] = (f2)b.y << 32 | b.x, o[3] = (f2)b.w << 32 | b.z;
+    } else {
+        unpack8(*reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(p) + at), o);
+    }
+}
+
+// One column's factor and summand of a norm as pairs; 1 and 0 where there are none.
+__device__ __forceinline__ void load_side8(const NormSide &n, int vec, f2 (&w)[4], f2 (&b)[4])
+{
+#pragma unroll
+    for (int j = 0; j < 4; j++) w[j] = f2_of(1.0f, 1.0f), b[j] = 0;
+    if (n.w) load_param8(n.w, n.fp32, (int64_t)vec * 8, w);
+    if (n.b) load_param8(n.b, n.fp32, (int64_t)vec * 8, b);
+}
+
+// ---- host -----------------------------------------------------------------------------------------
+// Lanes and vectors per lane of a row: the least of T * V >= cols / 8 with V = 3 or 4.
+inline void team_of(int64_t cols, int *log2_lanes, int *v)
+{
+    const int64_t nvec = cols / 8;
+    int l3 = 2, l4 = 2;
+    while ((3ll << l3) < nvec) l3++;
+    while ((4ll << l4) < nvec) l4++;
+    const bool three = (3ll << l3) <= (4ll << l4);
+    *log2_lanes = three ? l3 : l4;
+    *v = three ? 3 : 4;
+}
+
+// Blocks (one per SM of a B200) and the consecutive rows of one team.  By the shape alone: the backward pass's workspace is laid out by it.
+constexpr int kBlocks = 148;
+struct RowPlan {
+    int log2_lanes, v, blocks;
+    bool full;
+    int64_t rows_per_team;
+};
+inline RowPlan row_plan(int64_t rows, int64_t cols)
+{
+    RowPlan b;
+    team_of(cols, &b.log2_lanes, &b.v);
+    b.full = ((int64_t)b.v << b.log2_lanes) * 8 == cols;
+    const int64_t teams = kThreads >> b.log2_lanes, most = ceil_div(rows, teams);
+    b.rows_per_team = ceil_div(rows, (most < kBlocks ? most : kBlocks) * teams);
+    b.blocks = (int)ceil_div(ceil_div(rows, b.rows_per_team), teams);     // blocks that have rows
+    return b;
+}
+inline int64_t part_floats(const RowPlan &b, int64_t cols) { return (int64_t)b.blocks * 4 * cols; }
+inline int64_t slot_floats(const RowPlan &b, int64_t cols, int64_t gates) { return gates > 1 ? ((int64_t)b.blocks * (kThreads >> b.log2_lanes) + gates) * 2 * cols : 0; }
+
+inline mxfp4_status_t check_side(const mxfp4_norm_t &n)
+{
+    if (n.kind < MXFP4_NORM_NONE || n.kind > MXFP4_NORM_RMS) return MXFP4_INVALID_ARG;
+    if (n.kind == MXFP4_NORM_NONE) return MXFP4_OK;
+    if ((n.dtype != MXFP4_OUT_BF16 && n.dtype != MXFP4_OUT_FP32) || !(n.eps >= 0.0f)) return MXFP4_INVALID_ARG;
+    return aligned16(n.weight) && aligned16(n.bias) ? MXFP4_OK : MXFP4_MISALIGNED;
+}
+inline NormSide side_of(const mxfp4_norm_t &n) { return {n.weight, n.bias, n.dtype == MXFP4_OUT_FP32, n.kind == MXFP4_NORM_RMS, n.eps}; }
+
+// What the two directions check alike.
+inline mxfp4_status_t check_plan(const mxfp4_residual_norm_t *n)
+{
+    if (!n || n->rows < 0 || n->cols <= 0 || n->gates < 0) return MXFP4_INVALID_ARG;
+    if (n->x_dtype != MXFP4_OUT_BF16 && n->x_dtype != MXFP4_OUT_FP32) return MXFP4_INVALID_ARG;
+    if (n->cols % 32 != 0 || n->cols > kNormMaxCols || n->rows > 0x7FFFFFFF) return MXFP4_BAD_SHAPE;
+    mxfp4_status_t s;
+    if ((s = check_side(n->pre)) || (s = check_side(n->post))) return s;
+    if ((n->gates > 0) != (n->gate != nullptr)) return MXFP4_INVALID_ARG;
+    if (n->gate) {
+        if (n->gate_dtype != MXFP4_OUT_BF16 && n->gate_dtype != MXFP4_OUT_FP32) return MXFP4_INVALID_ARG;
+        if (n->rows % n->gates != 0) return MXFP4_BAD_SHAPE;
+        if (n->gates > 1 && n->ld_gate < n->cols) return MXFP4_BAD_SHAPE;
+        if (!aligned16(n->gate) || (n->gates > 1 && (n->ld_gate * dtype_bytes(n->gate_dtype)) % 16 != 0)) return MXFP4_MISALIGNED;
+    }
+    return MXFP4_OK;
+}
+
+// Outputs may lie over the input that is read in the same place (the same address and pitch), or apart from it.
+inline bool rows_over_or_apart(const Span &out, int64_t ldo, int64_t out_bytes, const Span &in, int64_t ldi, int64_t in_bytes)
+{
+    return !meet(out, in) || (out.lo == in.lo && ldo == ldi && out_bytes == in_bytes);
+}
+
+// Call f with the arguments as types, for a kernel's template arguments.
+template <class F> inline cudaError_t with_bools(bool a, bool b, bool c, F &&f)
+{
+    using T = std::true_type;
+    using N = std::false_type;
+    if (a) return b ? (c ? f(T(), T(), T()) : f(T(), T(), N())) : (c ? f(T(), N(), T()) : f(T(), N(), N()));
+    return b ? (c ? f(N(), T(), T()) : f(N(), T(), N())) : (c ? f(N(), N(), T()) : f(N(), N(), N()));
+}
+// Launches a kernel whose ring takes BYTES of shared memory.
+template <auto KERNEL, int BYTES, class P> inline cudaError_t launch_ring(int blocks, cudaStream_t st, const P &p)
+{
+    static bool attr_set[kMaxDevices];
+    const cudaError_t e = set_smem_once(attr_set, KERNEL, BYTES);
+    return e != cudaSuccess ? e : launch_pdl(KERNEL, (unsigned)blocks, 1, kThreads, BYTES, st, p);
+}
+template <class F> inline cudaError_t with_row(bool fp32, const RowPlan &plan, F &&f)
+{
+    return with_bools(fp32, plan.v == 4, plan.full, [&](auto wide, auto four, auto full) {
+        using XT = std::conditional_t<decltype(wide)::value, float, __nv_bfloat16>;
+        return f(XT(), std::integral_constant<int, decltype(four)::value ? 4 : 3>(), full);
+    });
+}
+
+}  // namespace mx
