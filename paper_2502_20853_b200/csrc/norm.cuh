@@ -4,10 +4,9 @@
 // The sums over a row go through shuffles and, where a team has several warps, through shared memory and a barrier of the team.
 // V is 3 or 4: with T a power of two these two reach every width within a third, and the usual widths (384 = 8 x 16 x 3, 768, 1024)
 // exactly; long lanes keep the shuffles few (five for 768 or 1024 columns).
-// One block of eight warps per SM; each team takes a run of consecutive rows, so that its lanes keep their columns: what belongs to a
-// column (weights, gates, sums over rows) stays in registers from row to row.  Eight warps cannot hide the memory's latency by
-// themselves; a lane's share of the next rows travels into shared memory meanwhile (cp.async into slots that only this lane reads: no
-// barriers).
+// One block per SM; each team takes a run of consecutive rows, so that its lanes keep their columns: what belongs to a column (weights,
+// a gate, sums over rows) is fetched once.  The few warps cannot hide the memory's latency by themselves; a lane's share of the next
+// rows travels into shared memory meanwhile (cp.async into slots that only this lane reads: no barriers).
 // FULL: T V vectors are exactly a row.  The kernels are bound by the instructions they issue, and without the masks of a partly filled
 // lane the loops over V are straight code.
 #pragma once
@@ -18,7 +17,7 @@
 namespace mx {
 
 constexpr int kNormMaxCols = 8192;
-constexpr int kThreads = 256;
+constexpr int kFwdThreads = 512, kBwdThreads = 256;
 
 // ---- a lane's ring of rows in shared memory ----------------------------------------------------
 __device__ __forceinline__ void async16(uint32_t dst, const void *src) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory"); }
@@ -37,25 +36,32 @@ __device__ __forceinline__ uint2 lds8(uint32_t at)
     asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at));
     return v;
 }
-// Eight elements of type T: slots of 16 bytes per lane, one (bf16) or two (fp32) of them.  A block's lanes lie side by side.
+// Eight elements of type T: slots of 16 bytes per lane, one (bf16) or two (fp32) of them.  The block's N lanes lie side by side.
 template <class T> constexpr int kSlots = sizeof(T) / 2;
-template <class T> __device__ __forceinline__ void async_row8(uint32_t slot, const T *src)
+template <class T, int N> __device__ __forceinline__ void async_row8(uint32_t slot, const T *src)
 {
     async16(slot, src);
-    if (sizeof(T) == 4) async16(slot + kThreads * 16, src + 4);
+    if (sizeof(T) == 4) async16(slot + N * 16, src + 4);
 }
-template <class T> __device__ __forceinline__ void ring_row8(uint32_t slot, f2 (&o)[4])
+template <class T, int N> __device__ __forceinline__ void ring_row8(uint32_t slot, f2 (&o)[4])
 {
     const uint4 a = lds16(slot);
     if (sizeof(T) == 2) {
         unpack8(a, o);
     } else {
-        const uint4 b = lds16(slot + kThreads * 16);
+        const uint4 b = lds16(slot + N * 16);
         o[0] = (f2)a.y << 32 | a.x, o[1] = (f2)a.w << 32 | a.z, o[2] = (f2)b.y << 32 | b.x, o[3] = (f2)b.w << 32 | b.z;
     }
 }
-// As many stages as fit beside `other` bytes, four at most.
-constexpr int ring_depth(int stage, int other) { return (220 * 1024 - other) / stage < 4 ? (220 * 1024 - other) / stage : 4; }
+constexpr int kRingBytes = 226 * 1024, kMostStages = 4;
+// Waits until at most `left` (0 to 3) of this lane's groups of copies are under way.
+__device__ __forceinline__ void async_wait_all_but(int left)
+{
+    if (left == 3) async_wait<3>();
+    else if (left == 2) async_wait<2>();
+    else if (left == 1) async_wait<1>();
+    else async_wait<0>();
+}
 __device__ __forceinline__ void zero8(f2 (&o)[4]) { o[0] = o[1] = o[2] = o[3] = 0; }
 
 // ---- teams --------------------------------------------------------------------------------------
@@ -84,10 +90,16 @@ __device__ __forceinline__ Team make_team(int log2_lanes, float4 *smem)
 template <int N>
 __device__ __forceinline__ void team_sum(Team &t, float (&v)[N])
 {
-    const int in_warp = min(t.lanes, 32);
-    for (int o = in_warp >> 1; o; o >>= 1)
+    if (t.lanes >= 32) {
 #pragma unroll
-        for (int k = 0; k < N; k++) v[k] += __shfl_xor_sync(0xFFFFFFFFu, v[k], o);
+        for (int o = 16; o; o >>= 1)
+#pragma unroll
+            for (int k = 0; k < N; k++) v[k] += __shfl_xor_sync(0xFFFFFFFFu, v[k], o);
+    } else {
+        for (int o = t.lanes >> 1; o; o >>= 1)
+#pragma unroll
+            for (int k = 0; k < N; k++) v[k] += __shfl_xor_sync(0xFFFFFFFFu, v[k], o);
+    }
     if (t.lanes > 32) {
         const int warps = t.lanes >> 5;
         float *s = reinterpret_cast<float *>(t.slots + t.turn * warps);
@@ -147,22 +159,23 @@ inline void team_of(int64_t cols, int *log2_lanes, int *v)
 // Blocks (one per SM of a B200) and the consecutive rows of one team.  By the shape alone: the backward pass's workspace is laid out by it.
 constexpr int kBlocks = 148;
 struct RowPlan {
-    int log2_lanes, v, blocks;
+    int log2_lanes, v, teams, blocks;
     bool full;
     int64_t rows_per_team;
 };
-inline RowPlan row_plan(int64_t rows, int64_t cols)
+inline RowPlan row_plan(int64_t rows, int64_t cols, int threads)
 {
     RowPlan b;
     team_of(cols, &b.log2_lanes, &b.v);
     b.full = ((int64_t)b.v << b.log2_lanes) * 8 == cols;
-    const int64_t teams = kThreads >> b.log2_lanes, most = ceil_div(rows, teams);
+    b.teams = threads >> b.log2_lanes;
+    const int64_t teams = b.teams, most = ceil_div(rows, teams);
     b.rows_per_team = ceil_div(rows, (most < kBlocks ? most : kBlocks) * teams);
     b.blocks = (int)ceil_div(ceil_div(rows, b.rows_per_team), teams);     // blocks that have rows
     return b;
 }
 inline int64_t part_floats(const RowPlan &b, int64_t cols) { return (int64_t)b.blocks * 4 * cols; }
-inline int64_t slot_floats(const RowPlan &b, int64_t cols, int64_t gates) { return gates > 1 ? ((int64_t)b.blocks * (kThreads >> b.log2_lanes) + gates) * 2 * cols : 0; }
+inline int64_t slot_floats(const RowPlan &b, int64_t cols, int64_t gates) { return gates > 1 ? ((int64_t)b.blocks * b.teams + gates) * 2 * cols : 0; }
 
 inline mxfp4_status_t check_side(const mxfp4_norm_t &n)
 {
@@ -205,12 +218,18 @@ template <class F> inline cudaError_t with_bools(bool a, bool b, bool c, F &&f)
     if (a) return b ? (c ? f(T(), T(), T()) : f(T(), T(), N())) : (c ? f(T(), N(), T()) : f(T(), N(), N()));
     return b ? (c ? f(N(), T(), T()) : f(N(), T(), N())) : (c ? f(N(), N(), T()) : f(N(), N(), N()));
 }
-// Launches a kernel whose ring takes BYTES of shared memory.
-template <auto KERNEL, int BYTES, class P> inline cudaError_t launch_ring(int blocks, cudaStream_t st, const P &p)
+// Stages of a ring: as many as there is room for beside `other` bytes.
+inline int ring_stages(size_t other, size_t stage)
+{
+    const size_t fit = (kRingBytes - other) / stage;
+    return (int)(fit < kMostStages ? fit : kMostStages);
+}
+// Launches a kernel of THREADS per block that may take up to kRingBytes of shared memory.
+template <auto KERNEL, int THREADS, class P> inline cudaError_t launch_ring(int blocks, size_t smem, cudaStream_t st, const P &p)
 {
     static bool attr_set[kMaxDevices];
-    const cudaError_t e = set_smem_once(attr_set, KERNEL, BYTES);
-    return e != cudaSuccess ? e : launch_pdl(KERNEL, (unsigned)blocks, 1, kThreads, BYTES, st, p);
+    const cudaError_t e = set_smem_once(attr_set, KERNEL, kRingBytes);
+    return e != cudaSuccess ? e : launch_pdl(KERNEL, (unsigned)blocks, 1, THREADS, smem, st, p);
 }
 template <class F> inline cudaError_t with_row(bool fp32, const RowPlan &plan, F &&f)
 {

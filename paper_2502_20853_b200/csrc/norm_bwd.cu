@@ -30,21 +30,21 @@ struct NormBwd {
 
 template <class XT, int V, bool EIGHT, bool NEED_F, bool PRE> struct BwdRing {
     // a stage: what is read of dx', dh, x^ (or x'), f^ (or f)
-    static constexpr int kX = sizeof(XT) * 8, kRow = kThreads * V;
+    static constexpr int kX = sizeof(XT) * 8, kRow = kBwdThreads * V;
     static constexpr int kDh = kX * kRow;
     static constexpr int kXh = kDh + (PRE ? 16 * kRow : 0);
     static constexpr int kFh = kXh + (PRE ? (EIGHT ? 8 : kX) * kRow : 0);
     static constexpr int kStage = kFh + (NEED_F ? (EIGHT ? 8 : 16) * kRow : 0);
     // behind the ring, also a lane's own: N_pre's weights, and s g w1 of the present gate, in FP32
     static constexpr int kW = PRE ? 32 * kRow : 0, kG = NEED_F ? 32 * kRow : 0;
-    static constexpr int kDepth = ring_depth(kStage, kW + kG);
+    static constexpr int kDepth = (kRingBytes - kW - kG) / kStage < kMostStages ? (kRingBytes - kW - kG) / kStage : kMostStages;
     static constexpr int kSums = 4 * 4 * 8 * kRow;       // at the end: four sums per column for each warp (team)
     static constexpr int kBytes = kDepth * kStage + kW + kG > kSums ? kDepth * kStage + kW + kG : kSums;
 };
 __device__ __forceinline__ void sts8(uint32_t slot, const f2 (&v)[4])
 {
     asm volatile("st.shared.v2.u64 [%0], {%1, %2};" ::"r"(slot), "l"(v[0]), "l"(v[1]) : "memory");
-    asm volatile("st.shared.v2.u64 [%0], {%1, %2};" ::"r"(slot + kThreads * 16), "l"(v[2]), "l"(v[3]) : "memory");
+    asm volatile("st.shared.v2.u64 [%0], {%1, %2};" ::"r"(slot + kBwdThreads * 16), "l"(v[2]), "l"(v[3]) : "memory");
 }
 
 // Each team takes a run of consecutive rows and keeps the sums over them of its lanes' columns in registers: of dh x^ and dh for N_pre's
@@ -53,15 +53,15 @@ __device__ __forceinline__ void sts8(uint32_t slot, const f2 (&v)[4])
 // They go to memory once per block, A and B of several gates once per team and gate; k_norm_bwd_finish adds them up.  BIAS: the sums of
 // dh and t are wanted (without biases they are not, and their registers are free).
 template <class XT, int V, bool FULL, bool EIGHT, bool NEED_F, bool POST, bool PRE, bool BIAS>
-__global__ void __launch_bounds__(kThreads, 1) k_norm_bwd(const __grid_constant__ NormBwd p)
+__global__ void __launch_bounds__(kBwdThreads, 1) k_norm_bwd(const __grid_constant__ NormBwd p)
 {
     using Ring = BwdRing<XT, V, EIGHT, NEED_F, PRE>;
-    constexpr int S = Ring::kDepth;
+    constexpr int N = kBwdThreads, S = Ring::kDepth;
     __shared__ float4 s_sum[2 * 8];
     extern __shared__ __align__(128) uint8_t s_ring[];
     pdl_launch_dependents();
     Team t = make_team(p.log2_lanes, s_sum);
-    const int64_t team = (int64_t)blockIdx.x * (kThreads >> p.log2_lanes) + t.id;
+    const int64_t team = (int64_t)blockIdx.x * (kBwdThreads >> p.log2_lanes) + t.id;
     const int64_t first = min(team * p.rows_per_team, p.rows), end = min(first + p.rows_per_team, p.rows);
     const int have = FULL ? V : max(0, min(V, (p.nvec - t.lane + t.lanes - 1) >> p.log2_lanes));
     const float inv = 1.0f / (float)p.cols;
@@ -75,15 +75,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_norm_bwd(const __grid_constant_
             for (int i = 0; i < V; i++)
                 if (i < have) {
                     const int c = (i * t.lanes + t.lane) * 8;
-                    if (p.dxo) async_row8(stage + at16 + i * kSlots<XT> * kThreads * 16, static_cast<const XT *>(p.dxo) + row * p.lddxo + c);
+                    if (p.dxo) async_row8<XT, N>(stage + at16 + i * kSlots<XT> * kBwdThreads * 16, static_cast<const XT *>(p.dxo) + row * p.lddxo + c);
                     if (PRE) {
-                        async_row8(stage + Ring::kDh + at16 + i * kThreads * 16, p.dh + row * p.lddh + c);
-                        if (EIGHT) async8(stage + Ring::kXh + at8 + i * kThreads * 8, p.xcodes + row * p.cols + c);
-                        else async_row8(stage + Ring::kXh + at16 + i * kSlots<XT> * kThreads * 16, static_cast<const XT *>(p.xo) + row * p.ldxo + c);
+                        async_row8<__nv_bfloat16, N>(stage + Ring::kDh + at16 + i * kBwdThreads * 16, p.dh + row * p.lddh + c);
+                        if (EIGHT) async8(stage + Ring::kXh + at8 + i * kBwdThreads * 8, p.xcodes + row * p.cols + c);
+                        else async_row8<XT, N>(stage + Ring::kXh + at16 + i * kSlots<XT> * kBwdThreads * 16, static_cast<const XT *>(p.xo) + row * p.ldxo + c);
                     }
                     if (NEED_F) {
-                        if (EIGHT) async8(stage + Ring::kFh + at8 + i * kThreads * 8, p.fcodes + row * p.cols + c);
-                        else async_row8(stage + Ring::kFh + at16 + i * kThreads * 16, p.f + row * p.ldf + c);
+                        if (EIGHT) async8(stage + Ring::kFh + at8 + i * kBwdThreads * 8, p.fcodes + row * p.cols + c);
+                        else async_row8<__nv_bfloat16, N>(stage + Ring::kFh + at16 + i * kBwdThreads * 16, p.f + row * p.ldf + c);
                     }
                 }
         }
@@ -122,7 +122,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_norm_bwd(const __grid_constant_
             f2 w[4], none[4];
             zero8(w);
             if (i < have) load_side8({p.pre.w, nullptr, p.pre.fp32, 0, 0.0f}, i * t.lanes + t.lane, w, none);
-            sts8(w_at + i * kThreads * 32, w);
+            sts8(w_at + i * kBwdThreads * 32, w);
         }
     }
     const auto new_gate = [&](int64_t gate) {
@@ -139,7 +139,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_norm_bwd(const __grid_constant_
 #pragma unroll
                 for (int j = 0; j < 4; j++) w[j] = f2_mul(w[j], f2_mul(g[j], f2_of(p.s, p.s)));
             }
-            sts8(g_at + i * kThreads * 32, w);
+            sts8(g_at + i * kBwdThreads * 32, w);
         }
     };
 
@@ -184,16 +184,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_norm_bwd(const __grid_constant_
         for (int i = 0; i < V; i++) xsc[i] = ckpt_scale(xs[i]), fsc[i] = ckpt_scale(fs[i]);
         fetch_small(row + 1);
         async_wait<S - 1>();
-        f2 xh[V][4], d[V][4], x[V][4];
+        f2 xh[V][4], d[V][4];
 #pragma unroll
         for (int i = 0; i < V; i++) {
             if (PRE) {
                 if (FULL || i < n) {
-                    ring_row8<__nv_bfloat16>(stage + Ring::kDh + at16 + i * kThreads * 16, d[i]);
+                    ring_row8<__nv_bfloat16, N>(stage + Ring::kDh + at16 + i * kBwdThreads * 16, d[i]);
                     if (EIGHT) {
-                        e4m3_to8(lds8(stage + Ring::kXh + at8 + i * kThreads * 8), xsc[i], xh[i]);
+                        e4m3_to8(lds8(stage + Ring::kXh + at8 + i * kBwdThreads * 8), xsc[i], xh[i]);
                     } else {
-                        ring_row8<XT>(stage + Ring::kXh + at16 + i * kSlots<XT> * kThreads * 16, xh[i]);
+                        ring_row8<XT, N>(stage + Ring::kXh + at16 + i * kSlots<XT> * kBwdThreads * 16, xh[i]);
                         const f2 m2 = f2_of(-pm0, -pm0), r2 = f2_of(pr0, pr0);
 #pragma unroll
                         for (int j = 0; j < 4; j++) xh[i][j] = f2_mul(f2_add(xh[i][j], m2), r2);
@@ -213,7 +213,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_norm_bwd(const __grid_constant_
 #pragma unroll
             for (int i = 0; i < V; i++) {
                 f2 w[4];
-                ring_row8<float>(w_at + i * kThreads * 32, w);
+                ring_row8<float, N>(w_at + i * kBwdThreads * 32, w);
                 c1[i] = c2[i] = 0;
 #pragma unroll
                 for (int j = 0; j < 4; j++) {
@@ -230,75 +230,58 @@ __global__ void __launch_bounds__(kThreads, 1) k_norm_bwd(const __grid_constant_
             team_sum(t, c);
         }
         const float m1 = p.pre.rms ? 0.0f : -c[0] * inv, m2 = -c[1] * inv;
+        const f2 k1 = f2_of(m1, m1), k2 = f2_of(m2, m2), kr = f2_of(pr0, pr0), ka = f2_of(p.a, p.a), ks = f2_of(p.s, p.s);
+        f2 e1[V], e2[V];
+        XT *const dx = static_cast<XT *>(p.dx) + row * p.lddx + t.lane * 8;
 #pragma unroll
         for (int i = 0; i < V; i++) {
-            if (p.dxo && (FULL ? live : i < n)) ring_row8<XT>(stage + at16 + i * kSlots<XT> * kThreads * 16, x[i]);
-            else zero8(x[i]);
-        }
-        if (PRE) {
-            const f2 a1 = f2_of(m1, m1), a2 = f2_of(m2, m2), r2 = f2_of(pr0, pr0);
+            const bool on = FULL ? live : i < n;
+            f2 x[4];
+            zero8(x);
+            if (p.dxo && on) ring_row8<XT, N>(stage + at16 + i * kSlots<XT> * N * 16, x);
+            if (PRE && on) {
 #pragma unroll
-            for (int i = 0; i < V; i++)
-#pragma unroll
-                for (int j = 0; j < 4; j++)
-                    if (FULL || i < n) x[i][j] = f2_fma(r2, f2_fma(xh[i][j], a2, f2_add(d[i][j], a1)), x[i][j]);
-            if (FULL && !live) {
-#pragma unroll
-                for (int i = 0; i < V; i++) zero8(x[i]);
+                for (int j = 0; j < 4; j++) x[j] = f2_fma(kr, f2_fma(xh[i][j], k2, f2_add(d[i][j], k1)), x[j]);
             }
-        }
-        if (live) {
-            XT *o = static_cast<XT *>(p.dx) + row * p.lddx;
-            const f2 a2 = f2_of(p.a, p.a);
+            if (on) {
+                f2 y[4];
 #pragma unroll
-            for (int i = 0; i < V; i++)
-                if (FULL || i < n) {
-                    f2 y[4];
-#pragma unroll
-                    for (int j = 0; j < 4; j++) y[j] = f2_mul(x[i][j], a2);
-                    store8(o + (i * t.lanes + t.lane) * 8, y);
-                }
-        }
-        // the branch: f^ and the gradient of u, then of f
-        if (NEED_F) {
-#pragma unroll
-            for (int i = 0; i < V; i++) {
-                if (FULL || i < n) {
-                    if (EIGHT) {
-                        e4m3_to8(lds8(stage + Ring::kFh + at8 + i * kThreads * 8), fsc[i], xh[i]);
-                    } else {
-                        ring_row8<__nv_bfloat16>(stage + Ring::kFh + at16 + i * kThreads * 16, xh[i]);
-                        if (POST) {
-                            const f2 n2 = f2_of(-qm0, -qm0), r2 = f2_of(qr0, qr0);
-#pragma unroll
-                            for (int j = 0; j < 4; j++) xh[i][j] = f2_mul(f2_add(xh[i][j], n2), r2);
-                        }
-                    }
-                } else {
+                for (int j = 0; j < 4; j++) y[j] = f2_mul(x[j], ka);
+                store8(dx + i * t.lanes * 8, y);
+            }
+            // the branch: from here on xh is f^, and d the gradient of f^, then of f
+            e1[i] = e2[i] = 0;
+            if (NEED_F) {
+                if (!on) {
                     zero8(xh[i]);
+                } else if (EIGHT) {
+                    e4m3_to8(lds8(stage + Ring::kFh + at8 + i * N * 8), fsc[i], xh[i]);
+                } else {
+                    ring_row8<__nv_bfloat16, N>(stage + Ring::kFh + at16 + i * N * 16, xh[i]);
+                    if (POST) {
+                        const f2 n2 = f2_of(-qm0, -qm0), r2 = f2_of(qr0, qr0);
+#pragma unroll
+                        for (int j = 0; j < 4; j++) xh[i][j] = f2_mul(f2_add(xh[i][j], n2), r2);
+                    }
                 }
-            }
-            if (FULL && !live) {
-#pragma unroll
-                for (int i = 0; i < V; i++) zero8(xh[i]);
-            }
-            f2 e1[V], e2[V];
-#pragma unroll
-            for (int i = 0; i < V; i++) {
                 f2 w[4];
-                ring_row8<float>(g_at + i * kThreads * 32, w);
-                e1[i] = e2[i] = 0;
+                ring_row8<float, N>(g_at + i * N * 32, w);
 #pragma unroll
                 for (int j = 0; j < 4; j++) {
-                    B[i][j] = f2_fma(x[i][j], xh[i][j], B[i][j]);
-                    if (BIAS) A[i][j] = f2_add(x[i][j], A[i][j]);
-                    x[i][j] = f2_mul(x[i][j], w[j]);
+                    B[i][j] = f2_fma(x[j], xh[i][j], B[i][j]);
+                    if (BIAS) A[i][j] = f2_add(x[j], A[i][j]);
+                    d[i][j] = f2_mul(x[j], w[j]);
                     if (POST) {
-                        e1[i] = j ? f2_add(e1[i], x[i][j]) : x[i][j];
-                        e2[i] = j ? f2_fma(x[i][j], xh[i][j], e2[i]) : f2_mul(x[i][j], xh[i][j]);
+                        e1[i] = j ? f2_add(e1[i], d[i][j]) : d[i][j];
+                        e2[i] = j ? f2_fma(d[i][j], xh[i][j], e2[i]) : f2_mul(d[i][j], xh[i][j]);
                     }
                 }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; j++) d[i][j] = f2_mul(x[j], ks);
             }
+        }
+        if (NEED_F) {
             if (POST) {
 #pragma unroll
                 for (int i = 1; i < V; i++) e1[0] = f2_add(e1[0], e1[i]), e2[0] = f2_add(e2[0], e2[i]);
@@ -309,20 +292,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_norm_bwd(const __grid_constant_
 #pragma unroll
                 for (int i = 0; i < V; i++)
 #pragma unroll
-                    for (int j = 0; j < 4; j++) x[i][j] = f2_mul(r2, f2_fma(xh[i][j], a2, f2_add(x[i][j], a1)));
+                    for (int j = 0; j < 4; j++) d[i][j] = f2_mul(r2, f2_fma(xh[i][j], a2, f2_add(d[i][j], a1)));
             }
-        } else {
-            const f2 s2 = f2_of(p.s, p.s);
-#pragma unroll
-            for (int i = 0; i < V; i++)
-#pragma unroll
-                for (int j = 0; j < 4; j++) x[i][j] = f2_mul(x[i][j], s2);
         }
         if (p.df && live) {
             __nv_bfloat16 *o = p.df + row * p.lddf;
 #pragma unroll
             for (int i = 0; i < V; i++)
-                if (FULL || i < n) store8(o + (i * t.lanes + t.lane) * 8, x[i]);
+                if (FULL || i < n) store8(o + (i * t.lanes + t.lane) * 8, d[i]);
         }
     }
 
@@ -331,7 +308,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_norm_bwd(const __grid_constant_
     async_wait<0>();
     __syncthreads();
     const int wide = max(t.lanes, 32);
-    const int parts = kThreads / wide, cols = p.cols;
+    const int parts = kBwdThreads / wide, cols = p.cols;
     float *const mine = reinterpret_cast<float *>(s_ring) + (int64_t)(threadIdx.x / wide) * 4 * cols;
     const auto leave = [&](f2 (&v)[V][4], int which) {
 #pragma unroll
@@ -349,7 +326,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_norm_bwd(const __grid_constant_
     if (with_f && BIAS) leave(A, 3);
     __syncthreads();
     float *part = p.part + (int64_t)blockIdx.x * 4 * cols;
-    for (int c = threadIdx.x * 4; c < 4 * cols; c += kThreads * 4) {
+    for (int c = threadIdx.x * 4; c < 4 * cols; c += kBwdThreads * 4) {
         const int which = c / cols;
         if ((which & 1) > BIAS || (which < 2 ? !PRE : !with_f)) continue;
         float4 v = make_float4(0, 0, 0, 0);
@@ -469,7 +446,7 @@ extern "C" {
 size_t mxfp4_residual_norm_workspace_bytes(int64_t rows, int64_t cols, int64_t gates)
 {
     if (rows <= 0 || cols <= 0 || cols > kNormMaxCols || gates < 0) return 0;
-    const RowPlan b = row_plan(rows, cols);
+    const RowPlan b = row_plan(rows, cols, kBwdThreads);
     return (size_t)(part_floats(b, cols) + slot_floats(b, cols, gates)) * 4;
 }
 
@@ -506,7 +483,7 @@ mxfp4_status_t mxfp4_residual_norm_bwd(const mxfp4_residual_norm_t *n, const mxf
     if (need_f && !eight && (s = check_rows(b->f_bf16, b->ldf, cols, MXFP4_OUT_BF16))) return s;
     if (!workspace) return MXFP4_INVALID_ARG;
     if (reinterpret_cast<uintptr_t>(workspace) & 255u) return MXFP4_MISALIGNED;
-    const RowPlan plan = row_plan(rows, cols);
+    const RowPlan plan = row_plan(rows, cols, kBwdThreads);
     if (workspace_bytes < (size_t)(part_floats(plan, cols) + slot_floats(plan, cols, n->gates)) * 4) return MXFP4_WORKSPACE_TOO_SMALL;
     {
         // dx and df are written row by row while later rows are still to be read
@@ -541,7 +518,7 @@ mxfp4_status_t mxfp4_residual_norm_bwd(const mxfp4_residual_norm_t *n, const mxf
             return with_bools(need_f, bias, false, [&](auto nf, auto bi, auto) -> cudaError_t {
                 constexpr bool F = decltype(nf)::value, B = decltype(bi)::value;
                 if constexpr ((Q && !F) || (!R && !F && (B || E))) return cudaErrorInvalidValue;     // does not occur
-                else return launch_ring<k_norm_bwd<XT, V, decltype(full)::value, E, F, Q, R, B>, BwdRing<XT, V, E, F, R>::kBytes>(plan.blocks, st, p);
+                else return launch_ring<k_norm_bwd<XT, V, decltype(full)::value, E, F, Q, R, B>, kBwdThreads>(plan.blocks, BwdRing<XT, V, E, F, R>::kBytes, st, p);
             });
         });
     }));
