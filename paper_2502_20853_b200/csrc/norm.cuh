@@ -1,6 +1,6 @@
 // What the two directions of the residual addition between norms share: teams, the ring of rows, parameters, the host's plan.
 //
-// A team of T lanes (a power of two from 4 to 256) holds a row in registers, each lane V vectors of eight columns: vector v * T + t.
+// A team of T lanes (a power of two from 4 to 256) holds a row in registers, each lane V vectors of eight columns.
 // The sums over a row go through shuffles and, where a team has several warps, through shared memory and a barrier of the team.
 // V is 3 or 4: with T a power of two these two reach every width within a third, and the usual widths (384 = 8 x 16 x 3, 768, 1024)
 // exactly; long lanes keep the shuffles few (five for 768 or 1024 columns).
@@ -65,52 +65,47 @@ __device__ __forceinline__ void async_wait_all_but(int left)
 __device__ __forceinline__ void zero8(f2 (&o)[4]) { o[0] = o[1] = o[2] = o[3] = 0; }
 
 // ---- teams --------------------------------------------------------------------------------------
-struct Team {
-    int lanes, lane;     // of the team
-    int id;              // of the team in its block
+// L: its lanes of one warp (32, or fewer where a warp holds several teams).  Lane l of a team's warp w holds the vectors
+// 32 V w + i L + l, i < V.
+template <int L> struct Team {
+    int warps, lane;     // of the team; of the warp's part of it
+    int id, first_vec;   // of the team in its block; of the lane
+    bool leader;
     float4 *slots;       // several warps: where they leave their sums, two sets that take turns
     int turn;
+
+    __device__ __forceinline__ Team(int team_warps, int v, float4 *smem) : warps(team_warps), lane(threadIdx.x & (L - 1)), turn(0)
+    {
+        const int part = L < 32 ? threadIdx.x / L : threadIdx.x >> 5;     // of a team, in the block
+        id = L < 32 ? part : part / team_warps;
+        const int w = L < 32 ? 0 : part - id * team_warps;
+        first_vec = w * 32 * v + lane;
+        leader = first_vec == 0;
+        slots = smem + id * 2 * team_warps;
+    }
 };
 
 // Rows of which a team of several in a warp has none left take part in its shuffles; `turns` is the same for all teams of a warp.
-__device__ __forceinline__ int64_t turns_of(const Team &t, int64_t rows_per_team, int64_t first, int64_t end) { return t.lanes < 32 ? rows_per_team : end - first; }
-
-__device__ __forceinline__ Team make_team(int log2_lanes, float4 *smem)
-{
-    Team t;
-    t.lanes = 1 << log2_lanes;
-    t.lane = threadIdx.x & (t.lanes - 1);
-    t.id = threadIdx.x >> log2_lanes;
-    t.slots = smem + t.id * 2 * (t.lanes >> 5);
-    t.turn = 0;
-    return t;
-}
+template <int L> __device__ __forceinline__ int turns_of(int rows_per_team, int64_t first, int64_t end) { return L < 32 ? rows_per_team : (int)(end - first); }
 
 // The sums of N (1, 2) numbers over the lanes of the team, the same bits in each of them.  All lanes of the warp take part.
-template <int N>
-__device__ __forceinline__ void team_sum(Team &t, float (&v)[N])
+template <int N, int L>
+__device__ __forceinline__ void team_sum(Team<L> &t, float (&v)[N])
 {
-    if (t.lanes >= 32) {
 #pragma unroll
-        for (int o = 16; o; o >>= 1)
+    for (int o = L / 2; o; o >>= 1)
 #pragma unroll
-            for (int k = 0; k < N; k++) v[k] += __shfl_xor_sync(0xFFFFFFFFu, v[k], o);
-    } else {
-        for (int o = t.lanes >> 1; o; o >>= 1)
-#pragma unroll
-            for (int k = 0; k < N; k++) v[k] += __shfl_xor_sync(0xFFFFFFFFu, v[k], o);
-    }
-    if (t.lanes > 32) {
-        const int warps = t.lanes >> 5;
-        float *s = reinterpret_cast<float *>(t.slots + t.turn * warps);
+        for (int k = 0; k < N; k++) v[k] += __shfl_xor_sync(0xFFFFFFFFu, v[k], o);
+    if (L == 32 && t.warps > 1) {
+        float *s = reinterpret_cast<float *>(t.slots + t.turn * t.warps);
         t.turn ^= 1;     // a warp that is ahead writes the other set: nobody is more than one barrier ahead
-        if ((t.lane & 31) == 0)
+        if (t.lane == 0)
 #pragma unroll
-            for (int k = 0; k < N; k++) s[(t.lane >> 5) * 4 + k] = v[k];
-        asm volatile("bar.sync %0, %1;" ::"r"(t.id + 1), "r"(t.lanes) : "memory");
+            for (int k = 0; k < N; k++) s[((threadIdx.x >> 5) - t.id * t.warps) * 4 + k] = v[k];
+        asm volatile("bar.sync %0, %1;" ::"r"(t.id + 1), "r"(t.warps * 32) : "memory");
 #pragma unroll
         for (int k = 0; k < N; k++) v[k] = 0.0f;
-        for (int w = 0; w < warps; w++)
+        for (int w = 0; w < t.warps; w++)
 #pragma unroll
             for (int k = 0; k < N; k++) v[k] += s[w * 4 + k];
     }
@@ -159,16 +154,20 @@ inline void team_of(int64_t cols, int *log2_lanes, int *v)
 // Blocks (one per SM of a B200) and the consecutive rows of one team.  By the shape alone: the backward pass's workspace is laid out by it.
 constexpr int kBlocks = 148;
 struct RowPlan {
-    int log2_lanes, v, teams, blocks;
+    int lanes, v, teams, blocks;    // lanes of a team, vectors of a lane, teams of a block
     bool full;
     int64_t rows_per_team;
+
+    int warps() const { return lanes <= 32 ? 1 : lanes / 32; }
 };
 inline RowPlan row_plan(int64_t rows, int64_t cols, int threads)
 {
     RowPlan b;
-    team_of(cols, &b.log2_lanes, &b.v);
-    b.full = ((int64_t)b.v << b.log2_lanes) * 8 == cols;
-    b.teams = threads >> b.log2_lanes;
+    int log2_lanes;
+    team_of(cols, &log2_lanes, &b.v);
+    b.lanes = 1 << log2_lanes;
+    b.full = (int64_t)b.v * b.lanes * 8 == cols;
+    b.teams = threads / b.lanes;
     const int64_t teams = b.teams, most = ceil_div(rows, teams);
     b.rows_per_team = ceil_div(rows, (most < kBlocks ? most : kBlocks) * teams);
     b.blocks = (int)ceil_div(ceil_div(rows, b.rows_per_team), teams);     // blocks that have rows
@@ -231,11 +230,14 @@ template <auto KERNEL, int THREADS, class P> inline cudaError_t launch_ring(int 
     const cudaError_t e = set_smem_once(attr_set, KERNEL, kRingBytes);
     return e != cudaSuccess ? e : launch_pdl(KERNEL, (unsigned)blocks, 1, THREADS, smem, st, p);
 }
-template <class F> inline cudaError_t with_row(bool fp32, const RowPlan &plan, F &&f)
+template <class F> inline cudaError_t with_lanes(const RowPlan &plan, F &&f)     // f(lanes of a warp's part of a team, vectors, full)
 {
-    return with_bools(fp32, plan.v == 4, plan.full, [&](auto wide, auto four, auto full) {
-        using XT = std::conditional_t<decltype(wide)::value, float, __nv_bfloat16>;
-        return f(XT(), std::integral_constant<int, decltype(four)::value ? 4 : 3>(), full);
+    return with_bools(plan.v == 4, plan.full, false, [&](auto four, auto full, auto) {
+        const std::integral_constant<int, decltype(four)::value ? 4 : 3> v;
+        return plan.lanes == 4    ? f(std::integral_constant<int, 4>(), v, full)
+               : plan.lanes == 8  ? f(std::integral_constant<int, 8>(), v, full)
+               : plan.lanes == 16 ? f(std::integral_constant<int, 16>(), v, full)
+                                  : f(std::integral_constant<int, 32>(), v, full);
     });
 }
 

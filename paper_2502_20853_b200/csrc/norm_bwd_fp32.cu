@@ -1,0 +1,8 @@
+// Residual addition between two norms, backward: the kernel for rows of fp32 with checkpoints.
+#include "norm_bwd.cuh"
+
+namespace mx {
+
+template cudaError_t launch_norm_bwd<float, true>(const NormBwd &, const RowPlan &, bool, bool, bool, cudaStream_t);
+
+}  // namespace mx

@@ -1,339 +1,10 @@
-// Residual addition between two norms, forward.
-#include "norm.cuh"
+// Residual addition between two norms, forward: the entry point, and the kernel for rows of bf16.
+#include "norm_fwd.cuh"
 
 namespace mx {
 
-struct NormFwd {
-    const void *x;
-    const __nv_bfloat16 *f;
-    void *xo;
-    __nv_bfloat16 *h;
-    int64_t ldx, ldf, ldxo, ldh;
-    NormSide pre, post;
-    const void *gate;
-    int64_t ldg;
-    uint32_t rows_per_gate;
-    int gate_fp32, several;     // several gates
-    int has_cw, has_cb;         // f^ has a factor other than s, a summand
-    int stages;                 // of the ring
-    float a, s;
-    float *stats;
-    CkptOut xc, fc;
-    uint8_t *hq, *hq_scales;
-    uint32_t hq_tf_add;
-    int nblk4;
-    int64_t rows, rows_per_team;
-    int cols, nvec, log2_lanes;
-    uint32_t *dev_status;
-};
-
-// mean and 1 / sqrt(var + eps) of the row that the lanes hold (zeros behind its end), by two passes; then the row is normalized.
-// `have`: vectors that this lane holds of the row (all, where it is FULL).
-template <int V, bool FULL>
-__device__ __forceinline__ void normalize(Team &t, const NormSide &n, float inv, int have, f2 (&v)[V][4], float &mean, float &rstd)
-{
-    float s[1];
-    mean = 0.0f;
-    if (!n.rms) {
-        f2 acc[V];
-#pragma unroll
-        for (int i = 0; i < V; i++) acc[i] = f2_add(f2_add(v[i][0], v[i][1]), f2_add(v[i][2], v[i][3]));
-#pragma unroll
-        for (int i = 1; i < V; i++) acc[0] = f2_add(acc[0], acc[i]);
-        s[0] = f2_sum(acc[0]);
-        team_sum(t, s);
-        mean = s[0] * inv;
-        const f2 m2 = f2_of(-mean, -mean);
-#pragma unroll
-        for (int i = 0; i < V; i++)
-#pragma unroll
-            for (int j = 0; j < 4; j++) v[i][j] = FULL || i < have ? f2_add(v[i][j], m2) : 0ull;     // zeros behind the row's end stay zeros
-    }
-    f2 acc[V];
-#pragma unroll
-    for (int i = 0; i < V; i++) {
-        acc[i] = f2_mul(v[i][0], v[i][0]);
-#pragma unroll
-        for (int j = 1; j < 4; j++) acc[i] = f2_fma(v[i][j], v[i][j], acc[i]);
-    }
-#pragma unroll
-    for (int i = 1; i < V; i++) acc[0] = f2_add(acc[0], acc[i]);
-    s[0] = f2_sum(acc[0]);
-    team_sum(t, s);
-    rstd = rsqrtf(s[0] * inv + n.eps);      // to 2^-23
-    const f2 r2 = f2_of(rstd, rstd);
-#pragma unroll
-    for (int i = 0; i < V; i++)
-#pragma unroll
-        for (int j = 0; j < 4; j++) v[i][j] = f2_mul(v[i][j], r2);
-}
-
-// The checkpoint of the row.  `n`: vectors of this lane that are written; `at`: where the lane's first one is, in eights of the matrix.
-template <int V, bool FULL>
-__device__ __forceinline__ bool row_ckpt(const CkptOut &o, const Team &t, int n, const f2 (&v)[V][4], int64_t at)
-{
-    uint32_t m[V], byte[V], worst = 0;
-    uint2 c[V];
-#pragma unroll
-    for (int i = 0; i < V; i++) m[i] = amax8(v[i]);
-#pragma unroll
-    for (int i = 0; i < V; i++) m[i] = group_max4(m[i]);
-#pragma unroll
-    for (int i = 0; i < V; i++) {
-        byte[i] = ckpt_scale_byte(m[i], o.tf_add);
-        c[i] = e4m3_x8(v[i], __uint_as_float((254u - byte[i]) << 23));
-        worst = max(worst, m[i]);
-    }
-    if (worst >= 0x7F800000u) {      // a group that is not finite: aside, it costs the others one comparison
-#pragma unroll
-        for (int i = 0; i < V; i++)
-            if (m[i] >= 0x7F800000u) c[i] = make_uint2(0, 0), byte[i] = 0xFFu;
-    }
-    if (n > 0) {
-        uint8_t *codes = o.codes + at * 8, *scales = o.scales + (at >> 2);
-#pragma unroll
-        for (int i = 0; i < V; i++)
-            if (FULL || i < n) {
-                *reinterpret_cast<uint2 *>(codes + i * t.lanes * 8) = c[i];
-                if ((t.lane & 3) == 0) scales[i * (t.lanes >> 2)] = (uint8_t)byte[i];
-            }
-    }
-    return n > 0 && worst >= 0x7F800000u;
-}
-
-template <class XT, int V, bool HAS_F> struct FwdRing {
-    static constexpr int N = kFwdThreads;
-    static constexpr int kF = kSlots<XT> * V * N * 16;                        // where f starts in a stage
-    static constexpr int kStage = kF + (HAS_F ? V * N * 16 : 0);
-};
-
-// A parameter of all columns in shared memory: two planes, the first and the second four of every eight columns.
-__device__ __forceinline__ void plane_put(float4 *plane, int nvec, int vec, const f2 (&v)[4])
-{
-    *reinterpret_cast<ulonglong2 *>(plane + vec) = make_ulonglong2(v[0], v[1]);
-    *reinterpret_cast<ulonglong2 *>(plane + nvec + vec) = make_ulonglong2(v[2], v[3]);
-}
-__device__ __forceinline__ void plane_get(const float4 *plane, int nvec, int vec, f2 (&v)[4])
-{
-    const ulonglong2 a = *reinterpret_cast<const ulonglong2 *>(plane + vec), b = *reinterpret_cast<const ulonglong2 *>(plane + nvec + vec);
-    v[0] = a.x, v[1] = a.y, v[2] = b.x, v[3] = b.y;
-}
-
-// x' = a x + (f^ cw + cb) [g], h = x^ pw + pb; cw = s w1 and cb = s b1, with one gate s g w1 and s g b1: the block keeps them in shared
-// memory as far as there are any (in registers they would leave room for eight warps instead of sixteen).
-template <class XT, int V, bool FULL, bool HAS_F, bool POST, bool PRE>
-__global__ void __launch_bounds__(kFwdThreads, 1) k_norm_fwd(const __grid_constant__ NormFwd p)
-{
-    using Ring = FwdRing<XT, V, HAS_F>;
-    constexpr int N = kFwdThreads;
-    __shared__ float4 s_sum[2 * (N / 32)];
-    extern __shared__ __align__(128) uint8_t s_ring[];
-    pdl_launch_dependents();
-    Team t = make_team(p.log2_lanes, s_sum);
-    const int64_t team = (int64_t)blockIdx.x * (N >> p.log2_lanes) + t.id;
-    const int64_t first = min(team * p.rows_per_team, p.rows), end = min(first + p.rows_per_team, p.rows);
-    const int have = FULL ? V : max(0, min(V, (p.nvec - t.lane + t.lanes - 1) >> p.log2_lanes));   // vectors of this lane
-    const float inv = 1.0f / (float)p.cols;
-    const int S = p.stages;
-    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(s_ring) + threadIdx.x * 16;
-    float4 *const plane_cw = reinterpret_cast<float4 *>(s_ring + S * Ring::kStage), *const plane_cb = plane_cw + (p.has_cw ? 2 * p.nvec : 0);
-    float4 *const plane_pw = plane_cb + (p.has_cb ? 2 * p.nvec : 0), *const plane_pb = plane_pw + (p.pre.w ? 2 * p.nvec : 0);
-    pdl_wait();
-
-    const XT *xp = static_cast<const XT *>(p.x) + first * p.ldx + t.lane * 8;       // of the row that is fetched next
-    const __nv_bfloat16 *fp = HAS_F ? p.f + first * p.ldf + t.lane * 8 : nullptr;
-    const auto fetch = [&](int64_t row, uint32_t stage) {
-        if (row < end) {
-#pragma unroll
-            for (int i = 0; i < V; i++)
-                if (FULL || i < have) async_row8<XT, N>(stage + i * kSlots<XT> * N * 16, xp + i * t.lanes * 8);
-            if (HAS_F) {
-#pragma unroll
-                for (int i = 0; i < V; i++)
-                    if (FULL || i < have) async_row8<__nv_bfloat16, N>(stage + Ring::kF + i * N * 16, fp + i * t.lanes * 8);
-                fp += p.ldf;
-            }
-            xp += p.ldx;
-        }
-        async_commit();
-    };
-    for (int k = 0; k < S - 1; k++) fetch(first + k, ring + k * Ring::kStage);
-
-    for (int vec = threadIdx.x; vec < p.nvec; vec += N) {
-        f2 w[4], b[4];
-        if (PRE) {
-            load_side8(p.pre, vec, w, b);
-            if (p.pre.w) plane_put(plane_pw, p.nvec, vec, w);
-            if (p.pre.b) plane_put(plane_pb, p.nvec, vec, b);
-        }
-        if (HAS_F && p.has_cw) {
-            f2 g[4];
-            load_side8(POST ? p.post : NormSide{}, vec, w, b);
-#pragma unroll
-            for (int j = 0; j < 4; j++) g[j] = f2_of(1.0f, 1.0f);
-            if (p.gate && !p.several) load_param8(p.gate, p.gate_fp32, vec * 8, g);
-#pragma unroll
-            for (int j = 0; j < 4; j++) {
-                g[j] = f2_mul(g[j], f2_of(p.s, p.s));
-                w[j] = f2_mul(w[j], g[j]), b[j] = f2_mul(b[j], g[j]);
-            }
-            plane_put(plane_cw, p.nvec, vec, w);
-            if (p.has_cb) plane_put(plane_cb, p.nvec, vec, b);
-        }
-    }
-    __syncthreads();
-
-    uint32_t gate = p.several ? (uint32_t)first / p.rows_per_gate : 0u;
-    uint32_t left = p.several ? p.rows_per_gate - ((uint32_t)first - gate * p.rows_per_gate) : 0u;   // rows of this gate still to come
-    bool bad = false;
-    int slot = 0;
-    int64_t at = first * p.nvec + t.lane;      // this row's place in a checkpoint
-    XT *xo = static_cast<XT *>(p.xo) + first * p.ldxo + t.lane * 8;
-    __nv_bfloat16 *h = p.h + first * p.ldh + t.lane * 8;
-    const int64_t turns = turns_of(t, p.rows_per_team, first, end);
-    for (int64_t k = 0; k < turns; k++) {
-        const int64_t row = first + k;
-        const bool live = row < end;
-        fetch(row + S - 1, ring + (slot == 0 ? S - 1 : slot - 1) * Ring::kStage);
-        const uint32_t stage = ring + slot * Ring::kStage;
-        slot = slot == S - 1 ? 0 : slot + 1;
-        if (HAS_F && p.several && live) {
-            if (left == 0) gate++, left = p.rows_per_gate;
-            left--;
-        }
-        const int n = live ? have : 0;
-        async_wait_all_but(S - 1);
-        f2 v[V][4];
-        if (HAS_F) {
-#pragma unroll
-            for (int i = 0; i < V; i++) {
-                if (FULL || i < n) ring_row8<__nv_bfloat16, N>(stage + Ring::kF + i * N * 16, v[i]);
-                else zero8(v[i]);
-            }
-            if (POST) {
-                float mean, rstd;
-                normalize<V, FULL>(t, p.post, inv, n, v, mean, rstd);
-                if (p.stats && live && t.lane == 0) p.stats[2 * p.rows + row] = mean, p.stats[3 * p.rows + row] = rstd;
-            }
-            if (p.fc.codes) bad |= row_ckpt<V, FULL>(p.fc, t, n, v, at);
-            if (p.has_cw) {
-#pragma unroll
-                for (int i = 0; i < V; i++) {
-                    f2 w[4];
-                    if (FULL || i < have) plane_get(plane_cw, p.nvec, i * t.lanes + t.lane, w);
-                    else zero8(w);
-#pragma unroll
-                    for (int j = 0; j < 4; j++) v[i][j] = f2_mul(v[i][j], w[j]);
-                }
-                if (p.has_cb) {
-#pragma unroll
-                    for (int i = 0; i < V; i++) {
-                        f2 w[4];
-                        if (FULL || i < have) plane_get(plane_cb, p.nvec, i * t.lanes + t.lane, w);
-                        else zero8(w);
-#pragma unroll
-                        for (int j = 0; j < 4; j++) v[i][j] = f2_add(v[i][j], w[j]);
-                    }
-                }
-                if (p.several && live) {
-#pragma unroll
-                    for (int i = 0; i < V; i++) {
-                        f2 g[4];
-                        if (FULL || i < have) load_param8(p.gate, p.gate_fp32, gate * p.ldg + (i * t.lanes + t.lane) * 8, g);
-                        else zero8(g);
-#pragma unroll
-                        for (int j = 0; j < 4; j++) v[i][j] = f2_mul(v[i][j], g[j]);
-                    }
-                }
-            } else {
-                const f2 s2 = f2_of(p.s, p.s);
-#pragma unroll
-                for (int i = 0; i < V; i++)
-#pragma unroll
-                    for (int j = 0; j < 4; j++) v[i][j] = f2_mul(v[i][j], s2);
-            }
-            const f2 a2 = f2_of(p.a, p.a);
-#pragma unroll
-            for (int i = 0; i < V; i++) {
-                f2 xx[4];
-                if (FULL || i < n) ring_row8<XT, N>(stage + i * kSlots<XT> * N * 16, xx);
-                else zero8(xx);
-#pragma unroll
-                for (int j = 0; j < 4; j++) v[i][j] = f2_fma(xx[j], a2, v[i][j]);
-            }
-            if (p.xo && live) {
-#pragma unroll
-                for (int i = 0; i < V; i++)
-                    if (FULL || i < n) store8(xo + i * t.lanes * 8, v[i]);
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < V; i++) {
-                if (FULL || i < n) ring_row8<XT, N>(stage + i * kSlots<XT> * N * 16, v[i]);
-                else zero8(v[i]);
-            }
-        }
-        if (PRE) {
-            float mean, rstd;
-            normalize<V, FULL>(t, p.pre, inv, n, v, mean, rstd);
-            if (p.stats && live && t.lane == 0) p.stats[row] = mean, p.stats[p.rows + row] = rstd;
-            if (p.xc.codes) bad |= row_ckpt<V, FULL>(p.xc, t, n, v, at);
-            if (p.pre.w) {
-#pragma unroll
-                for (int i = 0; i < V; i++) {
-                    f2 w[4];
-                    if (FULL || i < have) plane_get(plane_pw, p.nvec, i * t.lanes + t.lane, w);
-                    else zero8(w);
-#pragma unroll
-                    for (int j = 0; j < 4; j++) v[i][j] = f2_mul(v[i][j], w[j]);
-                }
-            }
-            if (p.pre.b) {
-#pragma unroll
-                for (int i = 0; i < V; i++) {
-                    f2 w[4];
-                    if (FULL || i < have) plane_get(plane_pb, p.nvec, i * t.lanes + t.lane, w);
-                    else zero8(w);
-#pragma unroll
-                    for (int j = 0; j < 4; j++) v[i][j] = f2_add(v[i][j], w[j]);
-                }
-            }
-            uint4 q[V];
-#pragma unroll
-            for (int i = 0; i < V; i++) q[i] = pack8(v[i]);
-            if (p.h && live) {
-#pragma unroll
-                for (int i = 0; i < V; i++)
-                    if (FULL || i < n) *reinterpret_cast<uint4 *>(h + i * t.lanes * 8) = q[i];
-            }
-            if (p.hq) {      // Q1 of the bf16 result, as the row-wise quantizer makes it
-#pragma unroll
-                for (int i = 0; i < V; i++) {
-                    const int vec = i * t.lanes + t.lane;
-                    uint32_t am = absmax_fold(absmax_fold(absmax_fold(absmax_fold(0u, q[i].x), q[i].y), q[i].z), q[i].w);
-                    am = group_max4(hmax_halves(absmax_fold_end(am)));
-                    const bool odd = am >= 0x7F80u;
-                    const uint32_t byte = odd ? 0xFFu : scale_byte_from_amax(am, p.hq_tf_add);
-                    const uint32_t c = odd ? 0u : rne8(q[i], inv_scale_bf16x2(byte));
-                    if (i < n) {
-                        bad |= odd;
-                        *reinterpret_cast<uint32_t *>(p.hq + row * (p.cols >> 1) + vec * 4) = c;
-                        if ((vec & 3) == 0) p.hq_scales[scale_offset(row, vec >> 2, p.nblk4)] = (uint8_t)byte;
-                    }
-                }
-            }
-            if (p.hq && live) {          // the scales' padding: blocks to a multiple of 4, rows to one of 128
-                const int nblk = p.cols >> 5;
-                if (nblk + t.lane < p.nblk4 * 4) p.hq_scales[scale_offset(row, nblk + t.lane, p.nblk4)] = 0x7F;
-                if (row == p.rows - 1)
-                    for (int64_t r = p.rows; r & 127; r++)
-                        for (int b = t.lane; b < p.nblk4 * 4; b += t.lanes) p.hq_scales[scale_offset(r, b, p.nblk4)] = 0x7F;
-            }
-        }
-        at += p.nvec, xo += p.ldxo, h += p.ldh;
-    }
-    if (bad && p.dev_status) atomicOr(p.dev_status, MXFP4_DEV_NONFINITE);
-}
+extern template cudaError_t launch_norm_fwd<float>(NormFwd &, const RowPlan &, bool, bool, bool, cudaStream_t);
+template cudaError_t launch_norm_fwd<__nv_bfloat16>(NormFwd &, const RowPlan &, bool, bool, bool, cudaStream_t);
 
 }  // namespace mx
 
@@ -374,7 +45,7 @@ mxfp4_status_t mxfp4_residual_norm_fwd(const mxfp4_residual_norm_t *n, const voi
         return MXFP4_INVALID_ARG;
     NormFwd p = {};
     const RowPlan plan = row_plan(rows, cols, kFwdThreads);
-    p.log2_lanes = plan.log2_lanes, p.rows_per_team = plan.rows_per_team;
+    p.warps = plan.warps(), p.teams = plan.teams, p.rows_per_team = plan.rows_per_team;
     p.x = x, p.f = static_cast<const __nv_bfloat16 *>(f_bf16), p.xo = x_out, p.h = static_cast<__nv_bfloat16 *>(h_bf16);
     p.ldx = ldx, p.ldf = ldf, p.ldxo = ldxo, p.ldh = ldh;
     p.pre = side_of(n->pre), p.post = side_of(n->post);
@@ -388,19 +59,7 @@ mxfp4_status_t mxfp4_residual_norm_fwd(const mxfp4_residual_norm_t *n, const voi
     if (hq) p.hq = static_cast<uint8_t *>(hq->data), p.hq_scales = hq->scales, p.hq_tf_add = scale_mode == MXFP4_SCALE_FLOOR ? 0u : 63u;
     p.rows = rows, p.cols = (int)cols, p.nvec = (int)(cols / 8), p.dev_status = dev_status;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    MX_CHECK_CUDA(with_row(n->x_dtype == MXFP4_OUT_FP32, plan, [&](auto xt, auto vv, auto full) {
-        using XT = decltype(xt);
-        constexpr int V = decltype(vv)::value;
-        return with_bools(has_f, post, pre, [&](auto f, auto q, auto r) -> cudaError_t {
-            constexpr bool F = decltype(f)::value, Q = decltype(q)::value, R = decltype(r)::value;
-            if constexpr (!F && (Q || !R)) return cudaErrorInvalidValue;     // refused above
-            else {
-                const size_t planes = (size_t)(p.has_cw + p.has_cb + (R && p.pre.w) + (R && p.pre.b)) * cols * 4;
-                p.stages = ring_stages(planes, FwdRing<XT, V, F>::kStage);
-                return launch_ring<k_norm_fwd<XT, V, decltype(full)::value, F, Q, R>, kFwdThreads>(plan.blocks, p.stages * FwdRing<XT, V, F>::kStage + planes, st, p);
-            }
-        });
-    }));
+    MX_CHECK_CUDA(n->x_dtype == MXFP4_OUT_FP32 ? launch_norm_fwd<float>(p, plan, has_f, post, pre, st) : launch_norm_fwd<__nv_bfloat16>(p, plan, has_f, post, pre, st));
     return MXFP4_OK;
 }
 
