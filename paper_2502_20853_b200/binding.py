@@ -23,8 +23,10 @@ class _NotBuilt:
 
 try:
     from . import _host
-    if getattr(_host, "interface", 0) != 2:      # what the calls below expect of it
+    if getattr(_host, "interface", 0) != 3:      # what the calls below expect of it
         _host = _NotBuilt()
+    else:
+        _host.types(torch.bfloat16, torch.float32)
 except ImportError:
     _host = _NotBuilt()
 
@@ -121,8 +123,10 @@ ALLOC_HOOK = None
 def _new(shape, dtype, device):
     if ALLOC_HOOK is not None:
         return ALLOC_HOOK(shape, dtype, device)
-    if len(shape) == 2:     # 1 us less than torch.empty with a shape of two
+    if len(shape) == 2:     # 1 us less than torch.empty
         return torch.empty_strided(shape, (shape[1], 1), dtype=dtype, device=device)
+    if len(shape) == 1:
+        return torch.empty_strided(shape, (1,), dtype=dtype, device=device)
     return torch.empty(shape, dtype=dtype, device=device)
 
 
@@ -208,7 +212,8 @@ def lib():
     L.mxfp4_residual_norm_workspace_bytes.restype = sz
     L.mxfp4_residual_norm_workspace_bytes.argtypes = [i64, i64, i64]
     # the entry points that _host calls
-    for name in ("linear_fwd_ex", "linear_bwd_ex", "quantize", "quantize_t", "qema_quantize"):
+    for name in ("linear_fwd_ex", "linear_bwd_ex", "quantize", "quantize_t", "qema_quantize", "residual_norm_fwd", "residual_norm_bwd",
+                 "residual_norm_workspace_bytes", "act_fwd", "act_bwd", "checkpoint_store", "checkpoint_load"):
         setattr(L, "at_" + name, C.cast(getattr(L, "mxfp4_" + name), C.c_void_p).value)
     _lib = L
     return L
@@ -686,71 +691,79 @@ def change_sums(cur, prev, out=None):
 
 # ---- 8-bit checkpoints of activations ----
 
-_OUT_OF = {torch.bfloat16: OUT_BF16, torch.float32: OUT_FP32}
-_DTYPES = (torch.bfloat16, torch.float32)
-
-
-def _rows(x, shape=None, dtype=None):
-    """A row-major matrix on the current device, of bf16 or fp32 (or of ``dtype``) and, where that is given, of ``shape``."""
-    assert x.is_cuda and x.get_device() == _device() and x.dtype in _DTYPES and x.dim() == 2 and x.stride(1) == 1
-    assert (dtype is None or x.dtype == dtype) and (shape is None or x.shape == shape), "another type or shape is expected"
-    return x
-
-
-def _here(t, dtype, shape):
-    """A contiguous tensor on the current device."""
-    assert t is None or (t.is_cuda and t.get_device() == _device() and t.dtype == dtype and t.shape == shape and t.is_contiguous())
-    return t
+_DTYPES = (torch.bfloat16, torch.float32)     # by MXFP4_OUT_*
 
 
 class Checkpoint:
-    """An activation kept in 8 bits: E4M3 ``codes`` (uint8 [rows, cols]) and one E8M0 byte per 32 columns, ``scales`` (uint8 [rows, cols / 32])."""
+    """An activation kept in 8 bits: E4M3 ``codes`` (uint8 [rows, cols]) and one E8M0 byte per 32 columns, ``scales`` (uint8 [rows, cols / 32]).
+    Those that the binding allocates itself share one buffer; ``codes`` and ``scales`` are views of it, made when they are asked for."""
 
-    __slots__ = ("codes", "scales")
+    __slots__ = ("shape", "_buf", "_codes", "_scales")
 
     def __init__(self, codes, scales):
         assert codes.dtype == torch.uint8 and scales.dtype == torch.uint8 and codes.dim() == 2 and codes.is_contiguous() and scales.is_contiguous()
-        assert codes.shape[1] % 32 == 0 and tuple(scales.shape) == (codes.shape[0], codes.shape[1] // 32) and codes.device == scales.device
-        self.codes, self.scales = codes, scales
+        rows, cols = codes.shape
+        assert cols % 32 == 0 and scales.shape == (rows, cols // 32) and codes.device == scales.device
+        self.shape, self._codes, self._scales = (rows, cols), codes, scales
 
     @staticmethod
     def empty(rows, cols, device="cuda"):
         assert cols % 32 == 0
-        return Checkpoint(_new((rows, cols), torch.uint8, device), _new((rows, cols // 32), torch.uint8, device))
+        if ALLOC_HOOK is not None:
+            return Checkpoint(_new((rows, cols), torch.uint8, device), _new((rows, cols // 32), torch.uint8, device))
+        self = Checkpoint.__new__(Checkpoint)
+        self.shape, self._codes, self._scales = (rows, cols), None, None
+        self._buf = torch.empty_strided((rows * cols + rows * cols // 32,), (1,), dtype=torch.uint8, device=device)
+        return self
 
     @property
-    def shape(self):
-        return self.codes.shape
+    def codes(self):
+        if self._codes is None:
+            rows, cols = self.shape
+            self._codes = self._buf.as_strided((rows, cols), (cols, 1), 0)
+        return self._codes
+
+    @property
+    def scales(self):
+        if self._scales is None:
+            rows, cols = self.shape
+            self._scales = self._buf.as_strided((rows, cols // 32), (cols // 32, 1), rows * cols)
+        return self._scales
 
     @property
     def device(self):
-        return self.codes.device
+        return (self._codes if self._codes is not None else self._buf).device
+
+    def _at(self, shape, device):
+        """The addresses of codes and scales; ``shape`` and ``device`` (an index): what the call expects."""
+        rows, cols = self.shape
+        t = self._codes if self._codes is not None else self._buf
+        assert (rows, cols) == shape and t.get_device() == device, "a checkpoint of another shape, or on another device"
+        p = t.data_ptr()
+        return p, self._scales.data_ptr() if self._scales is not None else (p if self._codes is None else self._buf.data_ptr()) + rows * cols
 
     def c(self):
-        return CCkpt(self.codes.data_ptr(), self.scales.data_ptr(), self.codes.shape[0], self.codes.shape[1])
-
-
-def _ckpt(c, shape=None):
-    if c is None:
-        return _NO_CKPT
-    assert c.codes.is_cuda and c.codes.get_device() == _device() and (shape is None or c.codes.shape == shape)
-    return c.c()
+        return CCkpt(*self._at(self.shape, self.device.index), *self.shape)
 
 
 def checkpoint_store(x, scale_mode=SCALE_TRUNCATION_FREE, out=None, dev_status=None):
     """The 8-bit checkpoint of x (bf16 or fp32 [rows, cols], cols a multiple of 32)."""
-    x = _rows(x)
-    out = out if out is not None else Checkpoint.empty(*x.shape, x.device)
-    _check("mxfp4_checkpoint_store", lib().mxfp4_checkpoint_store(x.data_ptr(), _OUT_OF[x.dtype], x.stride(0), _ckpt(out, x.shape), scale_mode, _ptr(dev_status), _stream()))
+    rows, cols = x.shape
+    if out is None:
+        out = Checkpoint.empty(rows, cols, x.device)
+    dev = _device()
+    _check("mxfp4_checkpoint_store",
+           _host.checkpoint_store(lib().at_checkpoint_store, dev, x, *out._at((rows, cols), dev), scale_mode, _ptr(dev_status), _stream()))
     return out
 
 
 def checkpoint_load(ckpt, out_dtype=OUT_BF16, out=None):
     """What a checkpoint stands for, as bf16 or fp32."""
     if out is None:
-        out = _new(tuple(ckpt.shape), _DTYPES[out_dtype], ckpt.device)
-    out = _rows(out, ckpt.shape)
-    _check("mxfp4_checkpoint_load", lib().mxfp4_checkpoint_load(_ckpt(ckpt), out.data_ptr(), _OUT_OF[out.dtype], out.stride(0), _stream()))
+        out = _new(ckpt.shape, _DTYPES[out_dtype], ckpt.device)
+    rows, cols = out.shape
+    dev = _device()
+    _check("mxfp4_checkpoint_load", _host.checkpoint_load(lib().at_checkpoint_load, dev, out, *ckpt._at((rows, cols), dev), 0, None, _stream()))
     return out
 
 
@@ -761,23 +774,25 @@ def _halves(act):
 def act_fwd(y, act=ACT_GELU, save=SAVE_8BIT, scale_mode=SCALE_TRUNCATION_FREE, out=None, ckpt=None, dev_status=None):
     """z = act(y), or act(y_a) y_b for the gated activations on y = [y_a, y_b], and the 8-bit checkpoint of y that act_bwd reads
     (``save=SAVE_NOTHING``: None).  y: bf16 [rows, cols] (gated: [rows, 2 cols])."""
-    y = _rows(y, dtype=torch.bfloat16)
-    assert save in (SAVE_NOTHING, SAVE_8BIT) and y.shape[1] % _halves(act) == 0
-    rows, cols = y.shape[0], y.shape[1] // _halves(act)
-    out = _rows(out if out is not None else _new((rows, cols), torch.bfloat16, y.device), (rows, cols), torch.bfloat16)
+    rows, cols = y.shape
+    assert save in (SAVE_NOTHING, SAVE_8BIT)
+    if out is None:
+        out = _new((rows, cols // _halves(act)), torch.bfloat16, y.device)
     if ckpt is None and save == SAVE_8BIT:
-        ckpt = Checkpoint.empty(*y.shape, y.device)
-    _check("mxfp4_act_fwd", lib().mxfp4_act_fwd(y.data_ptr(), y.stride(0), rows, cols, act, out.data_ptr(), out.stride(0), _ckpt(ckpt, y.shape), scale_mode,
-                                                _ptr(dev_status), _stream()))
+        ckpt = Checkpoint.empty(rows, cols, y.device)
+    dev = _device()
+    _check("mxfp4_act_fwd", _host.act_fwd(lib().at_act_fwd, dev, y, act, out, *(ckpt._at((rows, cols), dev) if ckpt is not None else (None, None)), scale_mode,
+                                          _ptr(dev_status), _stream()))
     return out, ckpt
 
 
 def act_bwd(dz, ckpt, act=ACT_GELU, out=None):
     """The gradient of y from that of z and the checkpoint of y."""
-    rows, ycols = ckpt.shape
-    dz = _rows(dz, (rows, ycols // _halves(act)), torch.bfloat16)
-    out = _rows(out if out is not None else _new((rows, ycols), torch.bfloat16, dz.device), (rows, ycols), torch.bfloat16)
-    _check("mxfp4_act_bwd", lib().mxfp4_act_bwd(dz.data_ptr(), dz.stride(0), _ckpt(ckpt), act, out.data_ptr(), out.stride(0), _stream()))
+    if out is None:
+        out = _new(ckpt.shape, torch.bfloat16, dz.device)
+    rows, cols = out.shape
+    dev = _device()
+    _check("mxfp4_act_bwd", _host.act_bwd(lib().at_act_bwd, dev, dz, *ckpt._at((rows, cols), dev), act, out, _stream()))
     return out
 
 
@@ -790,15 +805,6 @@ class Norm:
 
     def __init__(self, kind=NORM_LAYER, weight=None, bias=None, eps=1e-6):
         self.kind, self.weight, self.bias, self.eps = kind, weight, bias, eps
-
-    def c(self, cols):
-        w, b = self.weight, self.bias
-        one = w if w is not None else b
-        if one is None:
-            return CNorm(self.kind, 0, None, None, self.eps, 0)
-        for t in (w, b):    # of one type
-            _here(t, one.dtype, (cols,))
-        return CNorm(self.kind, _OUT_OF[one.dtype], _ptr(w), _ptr(b), self.eps, 0)
 
 
 class NormCtx:
@@ -815,16 +821,6 @@ class NormCtx:
 NormGrads = namedtuple("NormGrads", "dx df pre_weight pre_bias post_weight post_bias gate")
 
 
-def _residual_norm(rows, cols, x_dtype, pre, post, gate, residual_scale, branch_scale):
-    gates = ld = gd = 0
-    if gate is not None:
-        gate = _rows(gate if gate.dim() == 2 else gate.view(1, -1))
-        assert gate.shape[1] == cols
-        gates, ld, gd = gate.shape[0], gate.stride(0), _OUT_OF[gate.dtype]
-    return CResidualNorm(rows, cols, _OUT_OF[x_dtype], gd, residual_scale, branch_scale, pre.c(cols) if pre is not None else _NO_NORM,
-                         post.c(cols) if post is not None else _NO_NORM, _ptr(gate), gates, ld)
-
-
 def residual_norm_fwd(x, f=None, pre=None, post=None, gate=None, residual_scale=1.0, branch_scale=1.0, save=SAVE_8BIT, x_out=None, h=None, hq=None,
                       scale_mode=SCALE_TRUNCATION_FREE, dev_status=None):
     """The end of one branch of a transformer block and the start of the next, in one pass:
@@ -833,74 +829,75 @@ def residual_norm_fwd(x, f=None, pre=None, post=None, gate=None, residual_scale=
     for each rows / gates consecutive rows.  ``hq``: a QMat to fill with Q1(h), the next linear layer's operand (``h=False`` then leaves h itself out).
     ``save``: what the backward pass will read: the normalized rows in 8 bits, the inputs themselves (x_out and f, which must then stay as they
     are), or nothing.  Returns (x_out, h, NormCtx or None)."""
-    x = _rows(x)
     shape = rows, cols = x.shape
-    if f is not None:
-        f = _rows(f, shape, torch.bfloat16)
-        x_out = _rows(x_out if x_out is not None else _new(shape, x.dtype, x.device), shape, x.dtype)
-    else:
+    where = x.device
+    if f is None:
         assert x_out is None
+    elif x_out is None:
+        x_out = _new(shape, x.dtype, where)
     if h is False or pre is None:
         assert h is None or h is False
         h = None
-    else:
-        h = _rows(h if h is not None else _new(shape, torch.bfloat16, x.device), shape, torch.bfloat16)
-    plan = _residual_norm(rows, cols, x.dtype, pre, post, gate, residual_scale, branch_scale)
+    elif h is None:
+        h = _new(shape, torch.bfloat16, where)
+    dev = _device()
     kx = kf = stats = ctx = None
+    x_at = f_at = (None, None)
     if save != SAVE_NOTHING:
         assert save in (SAVE_8BIT, SAVE_INPUTS)
         keep_f = f is not None and (post is not None or gate is not None)
         if pre is not None or post is not None:
-            stats = _new((4, rows), torch.float32, x.device)
+            stats = _new((4, rows), torch.float32, where)
         if save == SAVE_8BIT:
-            kx = Checkpoint.empty(rows, cols, x.device) if pre is not None else None
-            kf = Checkpoint.empty(rows, cols, x.device) if keep_f else None
-            ctx = NormCtx(kx, kf, stats, pre, post, gate, residual_scale, branch_scale)
+            if pre is not None:
+                kx = Checkpoint.empty(rows, cols, where)
+                x_at = kx._at(shape, dev)
+            if keep_f:
+                kf = Checkpoint.empty(rows, cols, where)
+                f_at = kf._at(shape, dev)
         else:
-            ctx = NormCtx((x_out if f is not None else x) if pre is not None else None, f if keep_f else None, stats, pre, post, gate, residual_scale, branch_scale)
-    cq = hq.c() if hq is not None else None
-    _check("mxfp4_residual_norm_fwd",
-           lib().mxfp4_residual_norm_fwd(C.byref(plan), x.data_ptr(), x.stride(0), _ptr(f), f.stride(0) if f is not None else 0, _ptr(x_out),
-                                         x_out.stride(0) if x_out is not None else 0, _ptr(h), h.stride(0) if h is not None else 0,
-                                         C.byref(cq) if cq is not None else None, _ptr(stats), _ckpt(kx), _ckpt(kf), scale_mode, _ptr(dev_status), _stream()))
+            kx, kf = (x_out if f is not None else x) if pre is not None else None, f if keep_f else None
+        ctx = NormCtx(kx, kf, stats, pre, post, gate, residual_scale, branch_scale)
+    _check("mxfp4_residual_norm_fwd", _host.residual_norm_fwd(lib().at_residual_norm_fwd, dev, x, f, pre, post, gate, residual_scale, branch_scale, x_out, h, hq,
+                                                              _ptr(stats), *x_at, *f_at, scale_mode, _ptr(dev_status), _stream()))
     return x_out, h, ctx
 
 
 def residual_norm_workspace_bytes(rows, cols, gates):
-    return int(lib().mxfp4_residual_norm_workspace_bytes(rows, cols, gates))
+    return _host.residual_norm_workspace_bytes(lib().at_residual_norm_workspace_bytes, rows, cols, gates)
 
 
 def residual_norm_bwd(dh, dx_out, ctx, dx=None, df=None, workspace=None):
     """The gradients of residual_norm_fwd: NormGrads(dx, df, and in fp32 those of the norms' weights and biases [cols] and of the gate [gates, cols];
     None where there is no such thing).  dh: bf16, the gradient of h (None without ``pre``); dx_out: that of x_out from further on, in x's
-    type (None: 0).  ``df=False``: leaves it out (there was no f)."""
-    pre, post, gate = ctx.pre, ctx.post, ctx.gate
-    eight = isinstance(ctx.x if ctx.x is not None else ctx.f, Checkpoint)
+    type (None: 0; x's type is then dx's, or bf16).  ``df=False``: leaves it out (there was no f)."""
+    pre, post, gate, x, f = ctx.pre, ctx.post, ctx.gate, ctx.x, ctx.f
     given = dx_out if dx_out is not None else dh
     shape = rows, cols = given.shape
-    dev = given.device
-    x_dtype = dx_out.dtype if dx_out is not None else dx.dtype if dx is not None else ctx.x.dtype if not eight and ctx.x is not None else torch.bfloat16
-    if dh is not None:
-        dh = _rows(dh, shape, torch.bfloat16)
-    if dx_out is not None:
-        dx_out = _rows(dx_out, shape)
-    x, f = ctx.x, ctx.f
-    if not eight:
-        x, f = x if x is None else _rows(x, shape, x_dtype), f if f is None else _rows(f, shape, torch.bfloat16)
-    dx = _rows(dx if dx is not None else _new(shape, x_dtype, dev), shape, x_dtype)
-    df = None if df is False else _rows(df if df is not None else _new(shape, torch.bfloat16, dev), shape, torch.bfloat16)
-    plan = _residual_norm(rows, cols, x_dtype, pre, post, gate, ctx.residual_scale, ctx.branch_scale)
-    new = lambda yes, n=1: _new((n, cols) if n > 1 else (cols,), torch.float32, dev) if yes else None  # noqa: E731
-    gw, gb = new(pre is not None and pre.weight is not None), new(pre is not None and pre.bias is not None)
-    qw, qb = new(post is not None and post.weight is not None), new(post is not None and post.bias is not None)
-    gg = _new((max(plan.gates, 1), cols), torch.float32, dev) if gate is not None else None
+    where, dev = given.device, _device()
+    if dx is None:
+        dx = _new(shape, dx_out.dtype if dx_out is not None else torch.bfloat16, where)
+    if df is None:
+        df = _new(shape, torch.bfloat16, where)
+    elif df is False:
+        df = None
+    x_at = f_at = (None, None)
+    if isinstance(x, Checkpoint):
+        x, x_at = None, x._at(shape, dev)
+    if isinstance(f, Checkpoint):
+        f, f_at = None, f._at(shape, dev)
+    f32 = torch.float32
+    gw = _new((cols,), f32, where) if pre is not None and pre.weight is not None else None
+    gb = _new((cols,), f32, where) if pre is not None and pre.bias is not None else None
+    qw = _new((cols,), f32, where) if post is not None and post.weight is not None else None
+    qb = _new((cols,), f32, where) if post is not None and post.bias is not None else None
+    gates = 0 if gate is None else gate.shape[0] if gate.dim() == 2 else 1
+    gg = _new((gates, cols), f32, where) if gates else None
     if workspace is None:
-        workspace = _new((max(residual_norm_workspace_bytes(rows, cols, plan.gates), 256),), torch.uint8, dev)
-    b = CResidualNormBwd(_ptr(dh), dh.stride(0) if dh is not None else 0, _ptr(dx_out), dx_out.stride(0) if dx_out is not None else 0,
-                         _ptr(_here(ctx.stats, torch.float32, (4, rows))), *((_ckpt(x, shape), _ckpt(f, shape), None, 0, None, 0) if eight else
-                         (_NO_CKPT, _NO_CKPT, _ptr(x), x.stride(0) if x is not None else 0, _ptr(f), f.stride(0) if f is not None else 0)), dx.data_ptr(), dx.stride(0), _ptr(df),
-                         df.stride(0) if df is not None else 0, _ptr(gw), _ptr(gb), _ptr(qw), _ptr(qb), _ptr(gg))
-    _check("mxfp4_residual_norm_bwd", lib().mxfp4_residual_norm_bwd(C.byref(plan), C.byref(b), workspace.data_ptr(), workspace.numel(), _stream()))
+        workspace = _new((max(residual_norm_workspace_bytes(rows, cols, gates), 256),), torch.uint8, where)
+    _check("mxfp4_residual_norm_bwd",
+           _host.residual_norm_bwd(lib().at_residual_norm_bwd, dev, dh, dx_out, pre, post, gate, ctx.residual_scale, ctx.branch_scale, ctx.stats, x, f, *x_at, *f_at,
+                                   dx, df, _ptr(gw), _ptr(gb), _ptr(qw), _ptr(qb), _ptr(gg), workspace.data_ptr(), workspace.numel(), _stream()))
     return NormGrads(dx, df, gw, gb, qw, qb, gg)
 
 

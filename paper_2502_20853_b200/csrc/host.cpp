@@ -280,9 +280,256 @@ PyObject *h_qema(PyObject *, PyObject *const *a, Py_ssize_t n)
     return r.run([&] { return f(w, ema, (float)beta, update, nn, k, dst, mode, osc ? &o : nullptr, status, stream); });
 }
 
+// ---- tensors as arguments (the operators around the linear layers) ----
+// Attributes of a tensor read here cost a third of what they cost in Python (0.4 against 1.3 us for the five of a matrix).
+PyObject *g_get_device, *g_dtype, *g_shape, *g_stride, *g_kind, *g_weight, *g_bias, *g_eps, *g_bf16, *g_fp32;
+
+bool refuse(const char *what)
+{
+    if (!PyErr_Occurred()) PyErr_SetString(PyExc_AssertionError, what);
+    return false;
+}
+bool number(PyObject *o, int64_t &v)     // takes the reference
+{
+    if (!o) return false;
+    v = PyLong_AsLongLong(o);
+    Py_DECREF(o);
+    return v != -1 || !PyErr_Occurred();
+}
+bool entries(PyObject *o, int n, int64_t *v)     // takes the reference: a tuple of n numbers
+{
+    if (!o) return false;
+    bool ok = PyTuple_Check(o) && PyTuple_GET_SIZE(o) == n;
+    for (int i = 0; ok && i < n; i++) {
+        v[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(o, i));
+        ok = v[i] != -1 || !PyErr_Occurred();
+    }
+    Py_DECREF(o);
+    return ok;
+}
+struct Rows {
+    void *p = nullptr;
+    int64_t rows = 0, cols = 0, ld = 0;
+    int32_t dtype = 0;
+    bool given = false;
+};
+// dims 1 or 2 of bf16 or fp32 on `device`, the last one without gaps; one dimension counts as one row.
+bool tensor(PyObject *t, int64_t device, int dims, Rows &r)
+{
+    int64_t dev, size[2], step[2];
+    if (!number(PyObject_CallMethodNoArgs(t, g_get_device), dev)) return false;
+    if (dev != device) return refuse("a tensor on the current device is expected");
+    PyObject *dtype = PyObject_GetAttr(t, g_dtype);
+    if (!dtype) return false;
+    Py_DECREF(dtype);
+    if (dtype != g_bf16 && dtype != g_fp32) return refuse("a tensor of bf16 or fp32 is expected");
+    if (!entries(PyObject_GetAttr(t, g_shape), dims, size) || !entries(PyObject_CallMethodNoArgs(t, g_stride), dims, step))
+        return refuse(dims == 2 ? "a matrix is expected" : "a vector is expected");
+    if (size[dims - 1] > 1 && step[dims - 1] != 1) return refuse("the columns must lie side by side");
+    PyObject *a = PyObject_CallMethodNoArgs(t, g_data_ptr);
+    if (!a) return false;
+    r.p = reinterpret_cast<void *>((uintptr_t)PyLong_AsUnsignedLongLongMask(a));
+    Py_DECREF(a);
+    r.dtype = dtype == g_fp32 ? MXFP4_OUT_FP32 : MXFP4_OUT_BF16;
+    r.rows = dims == 2 ? size[0] : 1, r.cols = size[dims - 1];
+    r.ld = dims == 2 && size[0] > 1 ? step[0] : r.cols;     // of a single row torch may say anything
+    r.given = true;
+    return !PyErr_Occurred();
+}
+// A matrix argument of `like`'s shape (if that is given) and of a type (-1: any).
+bool matrix(PyObject *t, int64_t device, const Rows *like, int dtype, Rows &r)
+{
+    if (t == Py_None) return true;
+    if (!tensor(t, device, 2, r)) return false;
+    if (like && (r.rows != like->rows || r.cols != like->cols)) return refuse("a matrix of another shape is expected");
+    return dtype < 0 || r.dtype == dtype || refuse("a matrix of another type is expected");
+}
+bool norm_of(PyObject *o, int64_t device, int64_t cols, mxfp4_norm_t &n)
+{
+    n = mxfp4_norm_t{MXFP4_NORM_NONE, 0, nullptr, nullptr, 0.0f, 0u};
+    if (o == Py_None) return true;
+    int64_t kind;
+    if (!number(PyObject_GetAttr(o, g_kind), kind)) return false;
+    n.kind = (int32_t)kind;
+    PyObject *e = PyObject_GetAttr(o, g_eps);
+    if (!e) return false;
+    n.eps = (float)PyFloat_AsDouble(e);
+    Py_DECREF(e);
+    if (PyErr_Occurred()) return false;
+    Rows side[2];
+    PyObject *names[2] = {g_weight, g_bias};
+    for (int k = 0; k < 2; k++) {
+        PyObject *t = PyObject_GetAttr(o, names[k]);
+        if (!t) return false;
+        const bool ok = t == Py_None || tensor(t, device, 1, side[k]);
+        Py_DECREF(t);
+        if (!ok) return false;
+        if (side[k].given && side[k].cols != cols) return refuse("weight and bias have a number for each column");
+    }
+    if (side[0].given && side[1].given && side[0].dtype != side[1].dtype) return refuse("weight and bias have one type");
+    n.dtype = side[0].given ? side[0].dtype : side[1].dtype;
+    n.weight = side[0].p, n.bias = side[1].p;
+    return true;
+}
+// What residual_norm_fwd and _bwd share: arguments pre, post, gate, residual_scale, branch_scale at a[0 .. 4].
+bool plan_of(PyObject *const *a, int64_t device, const Rows &x, int32_t x_dtype, mxfp4_residual_norm_t &n)
+{
+    n = mxfp4_residual_norm_t{};
+    n.rows = x.rows, n.cols = x.cols, n.x_dtype = x_dtype;
+    if (!norm_of(a[0], device, x.cols, n.pre) || !norm_of(a[1], device, x.cols, n.post)) return false;
+    if (a[2] != Py_None) {
+        Rows g;
+        PyObject *shape = PyObject_GetAttr(a[2], g_shape);
+        if (!shape) return false;
+        const int dims = PyTuple_Check(shape) && PyTuple_GET_SIZE(shape) == 1 ? 1 : 2;
+        Py_DECREF(shape);
+        if (!tensor(a[2], device, dims, g)) return false;
+        if (g.cols != x.cols) return refuse("the gate has a number for each column");
+        n.gate = g.p, n.gates = g.rows, n.ld_gate = g.ld, n.gate_dtype = g.dtype;
+    }
+    n.residual_scale = (float)PyFloat_AsDouble(a[3]);
+    n.branch_scale = (float)PyFloat_AsDouble(a[4]);
+    return !PyErr_Occurred();
+}
+mxfp4_ckpt_t ckpt_of(Args &r, int i, const Rows &x) { return mxfp4_ckpt_t{r.ptr<uint8_t>(i), r.ptr<uint8_t>(i + 1), r.given(i) ? x.rows : 0, r.given(i) ? x.cols : 0}; }
+
+PyObject *h_norm_fwd(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    // entry, device, x, f, pre, post, gate, residual scale, branch scale, x_out, h, hq, stats, codes and scales of x^, of f^, scale_mode, status, stream
+    if (!counted("residual_norm_fwd", n, 20)) return nullptr;
+    Args r{a};
+    const auto f = reinterpret_cast<decltype(&mxfp4_residual_norm_fwd)>(r.ptr(0));
+    const int64_t device = r.i64(1);
+    Rows x, b, xo, h;
+    mxfp4_residual_norm_t plan;
+    if (a[2] == Py_None) refuse("x is expected");
+    if (a[2] == Py_None || !matrix(a[2], device, nullptr, -1, x) || !matrix(a[3], device, &x, MXFP4_OUT_BF16, b) || !plan_of(a + 4, device, x, x.dtype, plan) ||
+        !matrix(a[9], device, &x, x.dtype, xo) || !matrix(a[10], device, &x, MXFP4_OUT_BF16, h))
+        return nullptr;
+    const mxfp4_mat_t hq = r.dst(11);
+    const bool with_hq = r.given(11);
+    float *stats = r.ptr<float>(12);
+    const mxfp4_ckpt_t xc = ckpt_of(r, 13, x), fc = ckpt_of(r, 15, x);
+    const int32_t mode = r.i32(17);
+    auto *status = r.ptr<uint32_t>(18);
+    void *stream = r.ptr(19);
+    return r.run([&] { return f(&plan, x.p, x.ld, b.p, b.ld, xo.p, xo.ld, h.p, h.ld, with_hq ? &hq : nullptr, stats, xc, fc, mode, status, stream); });
+}
+
+PyObject *h_norm_bwd(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    // entry, device, dh, dx_out, pre, post, gate, residual scale, branch scale, stats, x, f, codes and scales of x^, of f^, dx, df, gradients of the
+    // norms (4) and of the gate, workspace, its bytes, stream
+    if (!counted("residual_norm_bwd", n, 26)) return nullptr;
+    Args r{a};
+    const auto f = reinterpret_cast<decltype(&mxfp4_residual_norm_bwd)>(r.ptr(0));
+    const int64_t device = r.i64(1);
+    Rows dx, dh, dxo, x, b, df, st;
+    mxfp4_residual_norm_t plan;
+    if (a[16] == Py_None) refuse("dx is expected");
+    if (a[16] == Py_None || !matrix(a[16], device, nullptr, -1, dx) || !matrix(a[2], device, &dx, MXFP4_OUT_BF16, dh) || !matrix(a[3], device, &dx, dx.dtype, dxo) ||
+        !plan_of(a + 4, device, dx, dx.dtype, plan) || !matrix(a[9], device, nullptr, MXFP4_OUT_FP32, st) || !matrix(a[10], device, &dx, dx.dtype, x) ||
+        !matrix(a[11], device, &dx, MXFP4_OUT_BF16, b) || !matrix(a[17], device, &dx, MXFP4_OUT_BF16, df))
+        return nullptr;
+    if (st.given && (st.rows != 4 || st.cols != dx.rows || (st.ld != st.cols && st.cols > 0))) {
+        refuse("the statistics are [4, rows], without gaps");
+        return nullptr;
+    }
+    mxfp4_residual_norm_bwd_t q{};
+    q.dh_bf16 = dh.p, q.lddh = dh.ld, q.dx_out = dxo.p, q.lddxo = dxo.ld, q.stats = static_cast<const float *>(st.p);
+    q.x_ckpt = ckpt_of(r, 12, dx), q.f_ckpt = ckpt_of(r, 14, dx);
+    q.x_out = x.p, q.ldxo = x.ld, q.f_bf16 = b.p, q.ldf = b.ld, q.dx = dx.p, q.lddx = dx.ld, q.df_bf16 = df.p, q.lddf = df.ld;
+    q.dw_pre = r.ptr<float>(18), q.db_pre = r.ptr<float>(19), q.dw_post = r.ptr<float>(20), q.db_post = r.ptr<float>(21), q.dgate = r.ptr<float>(22);
+    void *ws = r.ptr(23), *stream = r.ptr(25);
+    const uint64_t bytes = r.u64(24);
+    return r.run([&] { return f(&plan, &q, ws, bytes, stream); });
+}
+
+PyObject *h_norm_workspace(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    // entry, rows, cols, gates
+    if (!counted("residual_norm_workspace_bytes", n, 4)) return nullptr;
+    Args r{a};
+    const auto f = reinterpret_cast<decltype(&mxfp4_residual_norm_workspace_bytes)>(r.ptr(0));
+    const int64_t rows = r.i64(1), cols = r.i64(2), gates = r.i64(3);
+    return r.bad ? nullptr : PyLong_FromSize_t(f(rows, cols, gates));
+}
+
+PyObject *h_act_fwd(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    // entry, device, y, act, z, codes, scales, scale_mode, status, stream
+    if (!counted("act_fwd", n, 10)) return nullptr;
+    Args r{a};
+    const auto f = reinterpret_cast<decltype(&mxfp4_act_fwd)>(r.ptr(0));
+    const int64_t device = r.i64(1);
+    const int32_t act = r.i32(3);
+    Rows y, z;
+    if (!matrix(a[2], device, nullptr, MXFP4_OUT_BF16, y) || !matrix(a[4], device, nullptr, MXFP4_OUT_BF16, z)) return nullptr;
+    const int64_t halves = act == MXFP4_ACT_GEGLU || act == MXFP4_ACT_SWIGLU ? 2 : 1;
+    if (z.rows != y.rows || z.cols * halves != y.cols) {
+        refuse("z has y's shape, or half its columns where the activation is gated");
+        return nullptr;
+    }
+    const mxfp4_ckpt_t c = ckpt_of(r, 5, y);
+    const int32_t mode = r.i32(7);
+    auto *status = r.ptr<uint32_t>(8);
+    void *stream = r.ptr(9);
+    return r.run([&] { return f(y.p, y.ld, z.rows, z.cols, act, z.p, z.ld, c, mode, status, stream); });
+}
+
+PyObject *h_act_bwd(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    // entry, device, dz, codes, scales, act, dy, stream
+    if (!counted("act_bwd", n, 8)) return nullptr;
+    Args r{a};
+    const auto f = reinterpret_cast<decltype(&mxfp4_act_bwd)>(r.ptr(0));
+    const int64_t device = r.i64(1);
+    const int32_t act = r.i32(5);
+    Rows dz, dy;
+    if (!matrix(a[2], device, nullptr, MXFP4_OUT_BF16, dz) || !matrix(a[6], device, nullptr, MXFP4_OUT_BF16, dy)) return nullptr;
+    const int64_t halves = act == MXFP4_ACT_GEGLU || act == MXFP4_ACT_SWIGLU ? 2 : 1;
+    if (dz.rows != dy.rows || dz.cols * halves != dy.cols) {
+        refuse("dz has dy's shape, or half its columns where the activation is gated");
+        return nullptr;
+    }
+    const mxfp4_ckpt_t c = ckpt_of(r, 3, dy);
+    void *stream = r.ptr(7);
+    return r.run([&] { return f(dz.p, dz.ld, c, act, dy.p, dy.ld, stream); });
+}
+
+PyObject *h_ckpt(PyObject *, PyObject *const *a, Py_ssize_t n, bool store)
+{
+    // entry, device, the matrix, codes, scales, scale_mode, status, stream
+    if (!counted("checkpoint", n, 8)) return nullptr;
+    Args r{a};
+    const int64_t device = r.i64(1);
+    Rows x;
+    if (!matrix(a[2], device, nullptr, -1, x)) return nullptr;
+    const mxfp4_ckpt_t c = ckpt_of(r, 3, x);
+    const int32_t mode = r.i32(5);
+    auto *status = r.ptr<uint32_t>(6);
+    void *entry = r.ptr(0), *stream = r.ptr(7);
+    if (store) return r.run([&] { return reinterpret_cast<decltype(&mxfp4_checkpoint_store)>(entry)(x.p, x.dtype, x.ld, c, mode, status, stream); });
+    return r.run([&] { return reinterpret_cast<decltype(&mxfp4_checkpoint_load)>(entry)(c, x.p, x.dtype, x.ld, stream); });
+}
+PyObject *h_ckpt_store(PyObject *, PyObject *const *a, Py_ssize_t n) { return h_ckpt(nullptr, a, n, true); }
+PyObject *h_ckpt_load(PyObject *, PyObject *const *a, Py_ssize_t n) { return h_ckpt(nullptr, a, n, false); }
+
+// types(torch.bfloat16, torch.float32): what the tensors' dtypes are compared with
+PyObject *h_types(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (!counted("types", n, 2)) return nullptr;
+    Py_XSETREF(g_bf16, Py_NewRef(a[0]));
+    Py_XSETREF(g_fp32, Py_NewRef(a[1]));
+    Py_RETURN_NONE;
+}
+
 #define FAST(name, fn) {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(fn)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST("nbytes", h_nbytes), FAST("place", h_place), FAST("linear_fwd", h_linear_fwd), FAST("linear_bwd", h_linear_bwd),
-                         FAST("quantize", h_quantize), FAST("quantize_t", h_quantize_t), FAST("qema_quantize", h_qema), {nullptr, nullptr, 0, nullptr}};
+                         FAST("quantize", h_quantize), FAST("quantize_t", h_quantize_t), FAST("qema_quantize", h_qema),
+                         FAST("residual_norm_fwd", h_norm_fwd), FAST("residual_norm_bwd", h_norm_bwd), FAST("residual_norm_workspace_bytes", h_norm_workspace),
+                         FAST("act_fwd", h_act_fwd), FAST("act_bwd", h_act_bwd), FAST("checkpoint_store", h_ckpt_store), FAST("checkpoint_load", h_ckpt_load),
+                         FAST("types", h_types), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_host", nullptr, -1, methods};
 
 }  // namespace
@@ -298,9 +545,15 @@ PyMODINIT_FUNC PyInit__host()
     mat_type.tp_clear = mat_clear;
     mat_type.tp_members = mat_members;
     mat_type.tp_getset = mat_getset;
-    if (!g_data_ptr && !(g_data_ptr = PyUnicode_InternFromString("data_ptr"))) return nullptr;
+    const struct {
+        PyObject **at;
+        const char *name;
+    } names[] = {{&g_data_ptr, "data_ptr"}, {&g_get_device, "get_device"}, {&g_dtype, "dtype"}, {&g_shape, "shape"}, {&g_stride, "stride"},
+                 {&g_kind, "kind"}, {&g_weight, "weight"}, {&g_bias, "bias"}, {&g_eps, "eps"}};
+    for (const auto &n : names)
+        if (!*n.at && !(*n.at = PyUnicode_InternFromString(n.name))) return nullptr;
     if (PyType_Ready(&mat_type) < 0) return nullptr;
     PyObject *m = PyModule_Create(&module);
-    if (m && (PyModule_AddObjectRef(m, "Mat", reinterpret_cast<PyObject *>(&mat_type)) < 0 || PyModule_AddIntConstant(m, "interface", 2) < 0)) Py_CLEAR(m);
+    if (m && (PyModule_AddObjectRef(m, "Mat", reinterpret_cast<PyObject *>(&mat_type)) < 0 || PyModule_AddIntConstant(m, "interface", 3) < 0)) Py_CLEAR(m);
     return m;
 }
