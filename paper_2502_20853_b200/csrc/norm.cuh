@@ -174,7 +174,7 @@ inline RowPlan row_plan(int64_t rows, int64_t cols, int threads)
     return b;
 }
 inline int64_t part_floats(const RowPlan &b, int64_t cols) { return (int64_t)b.blocks * 4 * cols; }
-inline int64_t slot_floats(const RowPlan &b, int64_t cols, int64_t gates) { return gates > 1 ? ((int64_t)b.blocks * b.teams + gates) * 2 * cols : 0; }
+inline int64_t slot_floats(const RowPlan &b, int64_t cols, int64_t gates) { return gates > 1 ? ((int64_t)b.blocks * (b.teams + 1) + gates) * 2 * cols : 0; }
 
 inline mxfp4_status_t check_side(const mxfp4_norm_t &n)
 {

@@ -16,96 +16,97 @@ struct NormBwdFinish {
     int64_t ldg, gates;
     int gate_fp32, several;
     float s;
-    int blocks, pre, use_f, has_post, bias;
-    int64_t rows, rows_per_gate, rows_per_team;
-    int cols, split;          // split: lanes of rows that share a gate, a power of two
+    int blocks, pre, use_f, has_post;
+    int64_t rows, rows_per_gate, rows_per_block;
+    int cols, slices;         // slices of 128 columns
     float *dw_pre, *db_pre, *dw_post, *db_post, *dgate;
 };
 
-// Adds up what the blocks and teams have left, in a fixed order.  A block has 16 columns, 4 lanes of 4 columns by 64 lanes of rows.
+__device__ __forceinline__ void add4(float4 &a, const float4 &b) { a.x += b.x, a.y += b.y, a.z += b.z, a.w += b.w; }
+__device__ __forceinline__ float4 mul4(const float4 &a, const float4 &b) { return make_float4(a.x * b.x, a.y * b.y, a.z * b.z, a.w * b.w); }
+__device__ __forceinline__ float4 all4(float v) { return make_float4(v, v, v, v); }
+__device__ __forceinline__ float4 param4(const void *v, int fp32, int64_t at)
+{
+    if (fp32) return *reinterpret_cast<const float4 *>(static_cast<const float *>(v) + at);
+    const uint2 u = *reinterpret_cast<const uint2 *>(static_cast<const __nv_bfloat16 *>(v) + at);
+    return make_float4(bf16lo(u.x), bf16hi(u.x), bf16lo(u.y), bf16hi(u.y));
+}
+__device__ __forceinline__ float4 load4(const float *p) { return *reinterpret_cast<const float4 *>(p); }
+
+// dg = s (w1 B + b1 A)
+__device__ __forceinline__ float4 gate_gradient(const NormBwdFinish &p, int c, const float4 &B, const float4 &A)
+{
+    float4 o = B;
+    if (p.has_post && p.post.w) o = mul4(o, param4(p.post.w, p.post.fp32, c));
+    if (p.has_post && p.post.b) add4(o, mul4(A, param4(p.post.b, p.post.fp32, c)));
+    return mul4(o, all4(p.s));
+}
+
+// Adds up what the blocks and teams have left, in a fixed order.  Two kinds of blocks: the first cols / 16 take 16 columns each, 4 lanes of
+// 4 columns by 64 lanes of rows, for the sums over all rows; then, where there are several gates, one for each gate and 128 columns.
 __global__ void __launch_bounds__(256) k_norm_bwd_finish(const __grid_constant__ NormBwdFinish p)
 {
-    __shared__ float4 s_a[64][4], s_b[64][4];
+    __shared__ float4 s_v[8][4][4], s_g[8][2][32];
     pdl_launch_dependents();
     pdl_wait();
-    const int q = threadIdx.x & 3, r = threadIdx.x >> 2;
-    const int c = blockIdx.x * 16 + q * 4;
-    const auto add = [](float4 &a, const float4 &b) { a.x += b.x, a.y += b.y, a.z += b.z, a.w += b.w; };
-    // sums over the 64 lanes of rows, in every lane
-    const auto all_rows = [&](float4 &a, float4 &b) {
-        for (int o = 32; o; o >>= 1) {
-            __syncthreads();
-            s_a[r][q] = a, s_b[r][q] = b;
-            __syncthreads();
-            add(a, s_a[r ^ o][q]), add(b, s_b[r ^ o][q]);
-        }
-    };
-    const float4 zero = make_float4(0, 0, 0, 0);
-    if (p.pre && (p.dw_pre || p.db_pre)) {
-        float4 a = zero, b = zero;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    if ((int)blockIdx.x < p.cols / 16) {
+        const int q = threadIdx.x & 3, r = threadIdx.x >> 2, c = blockIdx.x * 16 + q * 4;
+        float4 v[4] = {all4(0), all4(0), all4(0), all4(0)};     // of dh x^, dh, t f^ (with several gates times g), t (the same)
+        const bool f = p.use_f && !p.several;
         for (int k = r; k < p.blocks; k += 64) {
-            const float *s = p.part + (int64_t)k * 4 * p.cols + c;
-            add(a, *reinterpret_cast<const float4 *>(s));
-            if (p.bias) add(b, *reinterpret_cast<const float4 *>(s + p.cols));
+            const float *at = p.part + (int64_t)k * 4 * p.cols + c;
+            if (p.pre) add4(v[0], load4(at)), add4(v[1], load4(at + p.cols));
+            if (f) add4(v[2], load4(at + 2 * p.cols)), add4(v[3], load4(at + 3 * p.cols));
         }
-        all_rows(a, b);
-        if (r == 0) {
-            if (p.dw_pre) *reinterpret_cast<float4 *>(p.dw_pre + c) = a;
-            if (p.db_pre) *reinterpret_cast<float4 *>(p.db_pre + c) = b;
-        }
-    }
-    if (!p.use_f || !(p.dw_post || p.db_post || p.dgate)) return;
-    float4 w = make_float4(1, 1, 1, 1), bias = zero;
-    const auto param = [&](const void *v, int fp32, int64_t at) {
-        if (fp32) return *reinterpret_cast<const float4 *>(static_cast<const float *>(v) + at);
-        const uint2 u = *reinterpret_cast<const uint2 *>(static_cast<const __nv_bfloat16 *>(v) + at);
-        return make_float4(bf16lo(u.x), bf16hi(u.x), bf16lo(u.y), bf16hi(u.y));
-    };
-    if (p.has_post && p.post.w) w = param(p.post.w, p.post.fp32, c);
-    if (p.has_post && p.post.b) bias = param(p.post.b, p.post.fp32, c);
-    const int in_turn = 64 / p.split;         // gates at a time
-    const int sub = r & (p.split - 1);
-    float4 cw = zero, cb = zero;              // sums over this lane's gates of g B and g A
-    for (int64_t g0 = 0; g0 < p.gates; g0 += in_turn) {
-        const int64_t g = g0 + r / p.split;
-        float4 B = zero, A = zero;
-        if (g < p.gates) {
-            if (p.several) {
-                const int64_t t0 = g * p.rows_per_gate / p.rows_per_team, t1 = ((g + 1) * p.rows_per_gate - 1) / p.rows_per_team;
-                for (int64_t k = t0 + sub; k <= t1; k += p.split) {
-                    const float *s = p.slots + (k + g) * 2 * (int64_t)p.cols + c;
-                    add(B, *reinterpret_cast<const float4 *>(s));
-                    if (p.bias) add(A, *reinterpret_cast<const float4 *>(s + p.cols));
-                }
-            } else {
-                for (int k = sub; k < p.blocks; k += p.split) {
-                    const float *s = p.part + (int64_t)k * 4 * p.cols + 2 * p.cols + c;
-                    add(B, *reinterpret_cast<const float4 *>(s));
-                    if (p.bias) add(A, *reinterpret_cast<const float4 *>(s + p.cols));
+        if (p.use_f && p.several && (p.dw_post || p.db_post))
+            for (int k = r; k < p.blocks; k += 64) {
+                const int64_t first = k * p.rows_per_block, end = first + p.rows_per_block < p.rows ? first + p.rows_per_block : p.rows;
+                for (uint32_t g = (uint32_t)first / (uint32_t)p.rows_per_gate; g <= (uint32_t)(end - 1) / (uint32_t)p.rows_per_gate; g++) {
+                    const float *at = p.slots + (int64_t)(k + g) * 2 * p.cols + c;
+                    const float4 w = param4(p.gate, p.gate_fp32, g * p.ldg + c);
+                    add4(v[2], mul4(load4(at), w)), add4(v[3], mul4(load4(at + p.cols), w));
                 }
             }
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+#pragma unroll
+            for (int o = 4; o < 32; o <<= 1)
+                add4(v[i], make_float4(__shfl_xor_sync(0xFFFFFFFFu, v[i].x, o), __shfl_xor_sync(0xFFFFFFFFu, v[i].y, o), __shfl_xor_sync(0xFFFFFFFFu, v[i].z, o),
+                                       __shfl_xor_sync(0xFFFFFFFFu, v[i].w, o)));
+            if (lane < 4) s_v[warp][i][lane] = v[i];
         }
-        for (int o = p.split >> 1; o; o >>= 1) {
-            __syncthreads();
-            s_a[r][q] = B, s_b[r][q] = A;
-            __syncthreads();
-            add(B, s_a[r ^ o][q]), add(A, s_b[r ^ o][q]);
+        __syncthreads();
+        if (threadIdx.x >= 4) return;
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            v[i] = s_v[0][i][q];
+#pragma unroll
+            for (int k = 1; k < 8; k++) add4(v[i], s_v[k][i][q]);
         }
-        if (g < p.gates && sub == 0) {
-            if (p.dgate)
-                *reinterpret_cast<float4 *>(p.dgate + g * p.cols + c) = make_float4(p.s * fmaf(w.x, B.x, bias.x * A.x), p.s * fmaf(w.y, B.y, bias.y * A.y),
-                                                                                    p.s * fmaf(w.z, B.z, bias.z * A.z), p.s * fmaf(w.w, B.w, bias.w * A.w));
-            const float4 gg = p.gate ? param(p.gate, p.gate_fp32, g * p.ldg + c) : make_float4(1, 1, 1, 1);
-            cw.x = fmaf(gg.x, B.x, cw.x), cw.y = fmaf(gg.y, B.y, cw.y), cw.z = fmaf(gg.z, B.z, cw.z), cw.w = fmaf(gg.w, B.w, cw.w);
-            cb.x = fmaf(gg.x, A.x, cb.x), cb.y = fmaf(gg.y, A.y, cb.y), cb.z = fmaf(gg.z, A.z, cb.z), cb.w = fmaf(gg.w, A.w, cb.w);
-        }
+        const auto put = [&](float *out, const float4 &x) { if (out) *reinterpret_cast<float4 *>(out + c) = x; };
+        put(p.dw_pre, v[0]), put(p.db_pre, v[1]);
+        if (f) put(p.dgate, gate_gradient(p, c, v[2], v[3]));
+        const float4 g = f && p.gate ? mul4(param4(p.gate, p.gate_fp32, c), all4(p.s)) : all4(p.s);
+        put(p.dw_post, mul4(v[2], g)), put(p.db_post, mul4(v[3], g));
+        return;
     }
-    if (!p.has_post) return;
-    all_rows(cw, cb);
-    if (r == 0) {
-        if (p.dw_post) *reinterpret_cast<float4 *>(p.dw_post + c) = make_float4(p.s * cw.x, p.s * cw.y, p.s * cw.z, p.s * cw.w);
-        if (p.db_post) *reinterpret_cast<float4 *>(p.db_post + c) = make_float4(p.s * cb.x, p.s * cb.y, p.s * cb.z, p.s * cb.w);
-    }
+    const int job = blockIdx.x - p.cols / 16;
+    const int64_t g = job / p.slices;
+    const int c = (job - (int)g * p.slices) * 128 + lane * 4;
+    const int64_t t0 = g * p.rows_per_gate / p.rows_per_block, t1 = ((g + 1) * p.rows_per_gate - 1) / p.rows_per_block;     // blocks
+    float4 B = all4(0), A = all4(0);
+    if (c < p.cols)
+        for (int64_t k = t0 + warp; k <= t1; k += 8) {
+            const float *at = p.slots + (k + g) * 2 * (int64_t)p.cols + c;
+            add4(B, load4(at)), add4(A, load4(at + p.cols));
+        }
+    s_g[warp][0][lane] = B, s_g[warp][1][lane] = A;
+    __syncthreads();
+    if (warp > 0 || c >= p.cols) return;
+#pragma unroll
+    for (int k = 1; k < 8; k++) add4(B, s_g[k][0][lane]), add4(A, s_g[k][1][lane]);
+    *reinterpret_cast<float4 *>(p.dgate + g * p.cols + c) = gate_gradient(p, c, B, A);
 }
 
 }  // namespace mx
@@ -178,21 +179,20 @@ mxfp4_status_t mxfp4_residual_norm_bwd(const mxfp4_residual_norm_t *n, const mxf
     p.gate = n->gate, p.ldg = n->ld_gate, p.gate_fp32 = n->gate_dtype == MXFP4_OUT_FP32;
     p.several = n->gates > 1, p.rows_per_gate = (uint32_t)(n->gates > 1 ? rows / n->gates : rows);
     p.a = n->residual_scale, p.s = n->branch_scale;
-    p.part = static_cast<float *>(workspace), p.slots = p.part + part_floats(plan, cols);
+    p.part = static_cast<float *>(workspace), p.slots = p.part + part_floats(plan, cols), p.heads = p.slots + ((int64_t)plan.blocks + n->gates) * 2 * cols;
     p.rows = rows, p.rows_per_team = plan.rows_per_team, p.cols = (int)cols, p.nvec = (int)(cols / 8), p.warps = plan.warps(), p.teams = plan.teams;
-    const bool bias = b->db_pre || b->db_post || (n->gate && n->post.bias && post);
     const auto go = n->x_dtype == MXFP4_OUT_FP32 ? (eight ? launch_norm_bwd<float, true> : launch_norm_bwd<float, false>)
                                                  : (eight ? launch_norm_bwd<__nv_bfloat16, true> : launch_norm_bwd<__nv_bfloat16, false>);
     MX_CHECK_CUDA(go(p, plan, need_f, post, pre, st));
     if (!b->dw_pre && !b->db_pre && !b->dw_post && !b->db_post && !b->dgate) return MXFP4_OK;
     NormBwdFinish e = {};
     e.part = p.part, e.slots = p.slots, e.post = p.post, e.gate = p.gate, e.ldg = p.ldg, e.gate_fp32 = p.gate_fp32;
-    e.gates = n->gates > 1 ? n->gates : 1, e.several = p.several, e.s = p.s, e.blocks = plan.blocks, e.pre = pre, e.use_f = need_f, e.has_post = post, e.bias = bias;
-    e.rows = rows, e.rows_per_gate = p.rows_per_gate, e.rows_per_team = plan.rows_per_team, e.cols = (int)cols;
-    e.split = 64;
-    while (e.split > 1 && 64 / e.split < e.gates) e.split >>= 1;
+    e.gates = n->gates > 1 ? n->gates : 1, e.several = p.several, e.s = p.s, e.blocks = plan.blocks, e.pre = pre, e.use_f = need_f, e.has_post = post;
+    e.rows = rows, e.rows_per_gate = p.rows_per_gate, e.rows_per_block = plan.rows_per_team * plan.teams, e.cols = (int)cols;
+    e.slices = (int)ceil_div(cols, 128);
     e.dw_pre = b->dw_pre, e.db_pre = b->db_pre, e.dw_post = b->dw_post, e.db_post = b->db_post, e.dgate = b->dgate;
-    MX_CHECK_CUDA(launch_pdl(k_norm_bwd_finish, (unsigned)(cols / 16), 1, 256, 0, st, e));
+    const int64_t blocks = cols / 16 + (e.several && b->dgate ? e.gates * e.slices : 0);
+    MX_CHECK_CUDA(launch_pdl(k_norm_bwd_finish, (unsigned)blocks, 1, 256, 0, st, e));
     return MXFP4_OK;
 }
 

@@ -24,7 +24,8 @@ struct NormBwd {
     int several;              // gates: A and B are kept apart by gate
     float a, s;
     float *part;              // [blocks][4][cols]: sums of dh x^, dh, t f^ (B), t (A)
-    float *slots;             // several gates: [team + gate][2][cols]: B and A of a team's rows of a gate
+    float *slots;             // several gates: [block + gate][2][cols]: B and A of a block's rows of a gate
+    float *heads;             // and [team][2][cols]: of a team's rows of its first gate, where it goes on to another
     int64_t rows, rows_per_team;
     int cols, nvec, warps, teams;     // of a team; of a block
 };
@@ -39,7 +40,7 @@ template <class XT, int V, bool EIGHT, bool NEED_F, bool PRE> struct BwdRing {
     // behind the ring, also a lane's own: N_pre's weights, and s g w1 of the present gate, in FP32
     static constexpr int kW = PRE ? 32 * kRow : 0, kG = NEED_F ? 32 * kRow : 0;
     static constexpr int kDepth = (kRingBytes - kW - kG) / kStage < kMostStages ? (kRingBytes - kW - kG) / kStage : kMostStages;
-    static constexpr int kSums = 4 * 4 * 8 * kRow;       // at the end: four sums per column for each warp (team)
+    static constexpr int kSums = 6 * 4 * 8 * kRow;       // at the end: up to six sums per column for each warp (team)
     static constexpr int kBytes = kDepth * kStage + kW + kG > kSums ? kDepth * kStage + kW + kG : kSums;
 };
 __device__ __forceinline__ void sts8(uint32_t slot, const f2 (&v)[4])
@@ -51,9 +52,8 @@ __device__ __forceinline__ void sts8(uint32_t slot, const f2 (&v)[4])
 // Each team takes a run of consecutive rows and keeps the sums over them of its lanes' columns in registers: of dh x^ and dh for N_pre's
 // gradients, and of t f^ and t (t the gradient of x' in all) for those of N_post and the gate:  with g constant over the rows of a gate,
 //     dg = s (w1 B + b1 A),   dw1 = s sum_g g B_g,   db1 = s sum_g g A_g,      B = sum t f^,  A = sum t.
-// They go to memory once per block, A and B of several gates once per team and gate; k_norm_bwd_finish adds them up.  BIAS: the sums of
-// dh and t are wanted (without biases they are not, and their registers are free).
-template <class XT, int L, int V, bool FULL, bool EIGHT, bool NEED_F, bool POST, bool PRE, bool BIAS>
+// They go to memory once per block, A and B of several gates once per block and gate; k_norm_bwd_finish adds them up. 
+template <class XT, int L, int V, bool FULL, bool EIGHT, bool NEED_F, bool POST, bool PRE>
 __global__ void __launch_bounds__(kBwdThreads, 1) k_norm_bwd(const __grid_constant__ NormBwd p)
 {
     using Ring = BwdRing<XT, V, EIGHT, NEED_F, PRE>;
@@ -150,14 +150,15 @@ __global__ void __launch_bounds__(kBwdThreads, 1) k_norm_bwd(const __grid_consta
     uint32_t gate = p.several ? (uint32_t)first / p.rows_per_gate : 0u;
     uint32_t left = p.several ? p.rows_per_gate - ((uint32_t)first - gate * p.rows_per_gate) : 0u;   // rows of this gate still to come
     if (NEED_F && first < end) new_gate(gate);
-    const auto flush = [&]() {
-        float *o = p.slots + (team + gate) * 2 * (int64_t)p.cols;
+    const uint32_t first_gate = gate;
+    const auto flush = [&]() {     // the rows of a gate are done and the team goes on: its first one is left to the block's end, any other is whole
+        float *o = gate == first_gate ? p.heads + team * 2 * p.cols : p.slots + ((int64_t)blockIdx.x + gate) * 2 * p.cols;
 #pragma unroll
         for (int i = 0; i < V; i++)
-            if (i < have) {
+            if (FULL || i < have) {
                 const int c = (i * L + t.first_vec) * 8;
                 store8(o + c, B[i]);
-                if (BIAS) store8(o + p.cols + c, A[i]);
+                store8(o + p.cols + c, A[i]);
                 zero8(B[i]), zero8(A[i]);
             }
     };
@@ -219,7 +220,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) k_norm_bwd(const __grid_consta
 #pragma unroll
                 for (int j = 0; j < 4; j++) {
                     sw[i][j] = f2_fma(d[i][j], xh[i][j], sw[i][j]);
-                    if (BIAS) sb[i][j] = f2_add(d[i][j], sb[i][j]);
+                    sb[i][j] = f2_add(d[i][j], sb[i][j]);
                     d[i][j] = f2_mul(d[i][j], w[j]);
                     c1[i] = j ? f2_add(c1[i], d[i][j]) : d[i][j];
                     c2[i] = j ? f2_fma(d[i][j], xh[i][j], c2[i]) : f2_mul(d[i][j], xh[i][j]);
@@ -270,7 +271,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) k_norm_bwd(const __grid_consta
 #pragma unroll
                 for (int j = 0; j < 4; j++) {
                     B[i][j] = f2_fma(x[j], xh[i][j], B[i][j]);
-                    if (BIAS) A[i][j] = f2_add(x[j], A[i][j]);
+                    A[i][j] = f2_add(x[j], A[i][j]);
                     d[i][j] = f2_mul(x[j], w[j]);
                     if (POST) {
                         e1[i] = j ? f2_add(e1[i], d[i][j]) : d[i][j];
@@ -304,7 +305,6 @@ __global__ void __launch_bounds__(kBwdThreads, 1) k_norm_bwd(const __grid_consta
         }
     }
 
-    if (NEED_F && p.several && first < end) flush();
     // the block's sums: teams of one warp by shuffles, then each warp's (team's) sums side by side in shared memory
     async_wait<0>();
     __syncthreads();
@@ -321,21 +321,54 @@ __global__ void __launch_bounds__(kBwdThreads, 1) k_norm_bwd(const __grid_consta
         }
     };
     const bool with_f = NEED_F && !p.several;
-    if (PRE) leave(sw, 0);
-    if (PRE && BIAS) leave(sb, 1);
-    if (with_f) leave(B, 2);
-    if (with_f && BIAS) leave(A, 3);
+    if (PRE) leave(sw, 0), leave(sb, 1);
+    if (with_f) leave(B, 2), leave(A, 3);
+    float *const last = reinterpret_cast<float *>(s_ring) + (int64_t)parts * 4 * cols;     // [team][2][cols]: of each team's last gate
+    if (NEED_F && p.several) {
+#pragma unroll
+        for (int i = 0; i < V; i++)
+            if (FULL || i < have) {
+                float *o = last + (int64_t)t.id * 2 * cols + (i * L + t.first_vec) * 8;
+                store8(o, B[i]);
+                store8(o + cols, A[i]);
+            }
+    }
     __syncthreads();
     float *part = p.part + (int64_t)blockIdx.x * 4 * cols;
     for (int c = threadIdx.x * 4; c < 4 * cols; c += kBwdThreads * 4) {
-        const int which = c / cols;
-        if ((which & 1) > BIAS || (which < 2 ? !PRE : !with_f)) continue;
+        if (c < 2 * cols ? !PRE : !with_f) continue;
         float4 v = make_float4(0, 0, 0, 0);
         for (int k = 0; k < parts; k++) {
             const float4 w = reinterpret_cast<const float4 *>(s_ring)[k * cols + c / 4];
             v.x += w.x, v.y += w.y, v.z += w.z, v.w += w.w;
         }
         *reinterpret_cast<float4 *>(part + c) = v;
+    }
+    if (NEED_F && p.several) {
+        // along the block's teams: what they have of one gate follows each other, a team's first gate, (gates that are its own,) its last
+        const int64_t row0 = (int64_t)blockIdx.x * p.teams * p.rows_per_team;
+        for (int c = threadIdx.x * 4; c < 2 * cols; c += kBwdThreads * 4) {
+            float4 v = make_float4(0, 0, 0, 0);
+            uint32_t now = (uint32_t)row0 / p.rows_per_gate;
+            const auto add = [&](const float *at) {
+                const float4 w = *reinterpret_cast<const float4 *>(at + c);
+                v.x += w.x, v.y += w.y, v.z += w.z, v.w += w.w;
+            };
+            const auto put = [&](uint32_t next) {
+                *reinterpret_cast<float4 *>(p.slots + ((int64_t)blockIdx.x + now) * 2 * cols + c) = v;
+                v = make_float4(0, 0, 0, 0);
+                now = next;
+            };
+            for (int k = 0; k < p.teams; k++) {
+                const int64_t from = row0 + k * p.rows_per_team, to = min(from + p.rows_per_team, p.rows);
+                if (from >= to) break;
+                const uint32_t a = (uint32_t)from / p.rows_per_gate, b = (uint32_t)(to - 1) / p.rows_per_gate;
+                if (a != now) put(a);
+                if (b != a) add(p.heads + ((int64_t)blockIdx.x * p.teams + k) * 2 * cols), put(b);
+                add(last + (int64_t)k * 2 * cols);
+            }
+            put(0);
+        }
     }
 }
 
@@ -347,7 +380,7 @@ template <class XT, bool EIGHT> cudaError_t launch_norm_bwd(const NormBwd &p, co
         return with_bools(need_f, post, pre, [&](auto f, auto q, auto r) -> cudaError_t {
             constexpr bool F = decltype(f)::value, Q = decltype(q)::value, R = decltype(r)::value;
             if constexpr ((Q && !F) || (!R && !F && EIGHT)) return cudaErrorInvalidValue;     // does not occur
-            else return launch_ring<k_norm_bwd<XT, L, V, decltype(full)::value, EIGHT, F, Q, R, true>, kBwdThreads>(plan.blocks, BwdRing<XT, V, EIGHT, F, R>::kBytes, st, p);
+            else return launch_ring<k_norm_bwd<XT, L, V, decltype(full)::value, EIGHT, F, Q, R>, kBwdThreads>(plan.blocks, BwdRing<XT, V, EIGHT, F, R>::kBytes, st, p);
         });
     });
 }
