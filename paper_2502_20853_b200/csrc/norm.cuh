@@ -1,9 +1,9 @@
 // What the two directions of the residual addition between norms share: teams, the ring of rows, parameters, the host's plan.
 //
-// A team of T lanes (a power of two from 4 to 256) holds a row in registers, each lane V vectors of eight columns.
-// The sums over a row go through shuffles and, where a team has several warps, through shared memory and a barrier of the team.
-// V is 3 or 4: with T a power of two these two reach every width within a third, and the usual widths (384 = 8 x 16 x 3, 768, 1024)
-// exactly; long lanes keep the shuffles few (five for 768 or 1024 columns).
+// A team of lanes (4, 8, 16, or a number of warps) holds a row in registers, each lane V vectors of eight columns.  The sums over a row go
+// through shuffles and, where a team has several warps, through shared memory and a barrier of the team.  V (2 to 4
+// backward, 3 or 4 forward) and the lanes are chosen so that a block's lanes have the most to do (row_plan); the usual widths are reached
+// exactly.
 // One block per SM; each team takes a run of consecutive rows, so that its lanes keep their columns: what belongs to a column (weights,
 // a gate, sums over rows) is fetched once.  The few warps cannot hide the memory's latency by themselves; a lane's share of the next
 // rows travels into shared memory meanwhile (cp.async into slots that only this lane reads: no barriers).
@@ -17,7 +17,9 @@
 namespace mx {
 
 constexpr int kNormMaxCols = 8192;
-constexpr int kFwdThreads = 512, kBwdThreads = 256;
+constexpr int kFwdThreads = 512;
+// Backward, by the vectors of a lane (their sums take 32 registers each): twelve warps with two, eight with three or four.
+constexpr int bwd_threads(int v) { return v == 2 ? 384 : 256; }
 
 // ---- a lane's ring of rows in shared memory ----------------------------------------------------
 __device__ __forceinline__ void async16(uint32_t dst, const void *src) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory"); }
@@ -62,6 +64,17 @@ __device__ __forceinline__ void async_wait_all_but(int left)
     else if (left == 1) async_wait<1>();
     else async_wait<0>();
 }
+// A parameter of all columns in shared memory: two planes, the first and the second four of every eight columns.
+__device__ __forceinline__ void plane_put(float4 *plane, int nvec, int vec, const f2 (&v)[4])
+{
+    *reinterpret_cast<ulonglong2 *>(plane + vec) = make_ulonglong2(v[0], v[1]);
+    *reinterpret_cast<ulonglong2 *>(plane + nvec + vec) = make_ulonglong2(v[2], v[3]);
+}
+__device__ __forceinline__ void plane_get(const float4 *plane, int nvec, int vec, f2 (&v)[4])
+{
+    const ulonglong2 a = *reinterpret_cast<const ulonglong2 *>(plane + vec), b = *reinterpret_cast<const ulonglong2 *>(plane + nvec + vec);
+    v[0] = a.x, v[1] = a.y, v[2] = b.x, v[3] = b.y;
+}
 __device__ __forceinline__ void zero8(f2 (&o)[4]) { o[0] = o[1] = o[2] = o[3] = 0; }
 
 // ---- teams --------------------------------------------------------------------------------------
@@ -86,6 +99,7 @@ template <int L> struct Team {
 };
 
 // Rows of which a team of several in a warp has none left take part in its shuffles; `turns` is the same for all teams of a warp.
+// (A warp that is in no team has no rows.)
 template <int L> __device__ __forceinline__ int turns_of(int rows_per_team, int64_t first, int64_t end) { return L < 32 ? rows_per_team : (int)(end - first); }
 
 // The sums of N (1, 2) numbers over the lanes of the team, the same bits in each of them.  All lanes of the warp take part.
@@ -139,18 +153,6 @@ __device__ __forceinline__ void load_side8(const NormSide &n, int vec, f2 (&w)[4
 }
 
 // ---- host -----------------------------------------------------------------------------------------
-// Lanes and vectors per lane of a row: the least of T * V >= cols / 8 with V = 3 or 4.
-inline void team_of(int64_t cols, int *log2_lanes, int *v)
-{
-    const int64_t nvec = cols / 8;
-    int l3 = 2, l4 = 2;
-    while ((3ll << l3) < nvec) l3++;
-    while ((4ll << l4) < nvec) l4++;
-    const bool three = (3ll << l3) <= (4ll << l4);
-    *log2_lanes = three ? l3 : l4;
-    *v = three ? 3 : 4;
-}
-
 // Blocks (one per SM of a B200) and the consecutive rows of one team.  By the shape alone: the backward pass's workspace is laid out by it.
 constexpr int kBlocks = 148;
 struct RowPlan {
@@ -160,14 +162,21 @@ struct RowPlan {
 
     int warps() const { return lanes <= 32 ? 1 : lanes / 32; }
 };
-inline RowPlan row_plan(int64_t rows, int64_t cols, int threads)
+// Of v to 4 vectors per lane, and the fewest lanes that hold a row then, whatever leaves the fewest of a block's vectors without work; of
+// several the shorter lanes backward (more warps), the longer ones forward (fewer shuffles).
+template <bool FWD> inline RowPlan row_plan(int64_t rows, int64_t cols)
 {
-    RowPlan b;
-    int log2_lanes;
-    team_of(cols, &log2_lanes, &b.v);
-    b.lanes = 1 << log2_lanes;
+    RowPlan b = {};
+    const int64_t nvec = cols / 8;
+    int best = 0;
+    for (int k = FWD ? 3 : 2; k <= 4; k++) {
+        const int threads = FWD ? kFwdThreads : bwd_threads(k);
+        int lanes = 4;
+        while (lanes * k < nvec) lanes += lanes < 32 ? lanes : 32;
+        const int teams = threads / lanes, used = (int)(teams * nvec * 1000 / (threads * k));     // in thousandths
+        if (teams > 0 && (FWD ? used >= best : used > best)) b.v = k, b.lanes = lanes, b.teams = teams, best = used;
+    }
     b.full = (int64_t)b.v * b.lanes * 8 == cols;
-    b.teams = threads / b.lanes;
     const int64_t teams = b.teams, most = ceil_div(rows, teams);
     b.rows_per_team = ceil_div(rows, (most < kBlocks ? most : kBlocks) * teams);
     b.blocks = (int)ceil_div(ceil_div(rows, b.rows_per_team), teams);     // blocks that have rows
@@ -230,15 +239,21 @@ template <auto KERNEL, int THREADS, class P> inline cudaError_t launch_ring(int 
     const cudaError_t e = set_smem_once(attr_set, KERNEL, kRingBytes);
     return e != cudaSuccess ? e : launch_pdl(KERNEL, (unsigned)blocks, 1, THREADS, smem, st, p);
 }
-template <class F> inline cudaError_t with_lanes(const RowPlan &plan, F &&f)     // f(lanes of a warp's part of a team, vectors, full)
+template <int V, class F> inline cudaError_t with_lanes_of(const RowPlan &plan, F &&f)
 {
-    return with_bools(plan.v == 4, plan.full, false, [&](auto four, auto full, auto) {
-        const std::integral_constant<int, decltype(four)::value ? 4 : 3> v;
+    return with_bools(plan.full, false, false, [&](auto full, auto, auto) {
+        const std::integral_constant<int, V> v;
         return plan.lanes == 4    ? f(std::integral_constant<int, 4>(), v, full)
                : plan.lanes == 8  ? f(std::integral_constant<int, 8>(), v, full)
                : plan.lanes == 16 ? f(std::integral_constant<int, 16>(), v, full)
                                   : f(std::integral_constant<int, 32>(), v, full);
     });
+}
+template <bool FWD, class F> inline cudaError_t with_lanes(const RowPlan &plan, F &&f)     // f(lanes of a warp's part of a team, vectors, full)
+{
+    if constexpr (!FWD)
+        if (plan.v == 2) return with_lanes_of<2>(plan, f);
+    return plan.v == 3 ? with_lanes_of<3>(plan, f) : with_lanes_of<4>(plan, f);
 }
 
 }  // namespace mx

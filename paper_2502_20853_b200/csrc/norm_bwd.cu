@@ -118,7 +118,7 @@ extern "C" {
 size_t mxfp4_residual_norm_workspace_bytes(int64_t rows, int64_t cols, int64_t gates)
 {
     if (rows <= 0 || cols <= 0 || cols > kNormMaxCols || gates < 0) return 0;
-    const RowPlan b = row_plan(rows, cols, kBwdThreads);
+    const RowPlan b = row_plan<false>(rows, cols);
     return (size_t)(part_floats(b, cols) + slot_floats(b, cols, gates)) * 4;
 }
 
@@ -155,7 +155,7 @@ mxfp4_status_t mxfp4_residual_norm_bwd(const mxfp4_residual_norm_t *n, const mxf
     if (need_f && !eight && (s = check_rows(b->f_bf16, b->ldf, cols, MXFP4_OUT_BF16))) return s;
     if (!workspace) return MXFP4_INVALID_ARG;
     if (reinterpret_cast<uintptr_t>(workspace) & 255u) return MXFP4_MISALIGNED;
-    const RowPlan plan = row_plan(rows, cols, kBwdThreads);
+    const RowPlan plan = row_plan<false>(rows, cols);
     if (workspace_bytes < (size_t)(part_floats(plan, cols) + slot_floats(plan, cols, n->gates)) * 4) return MXFP4_WORKSPACE_TOO_SMALL;
     {
         // dx and df are written row by row while later rows are still to be read

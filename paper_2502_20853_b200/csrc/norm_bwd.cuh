@@ -32,7 +32,7 @@ struct NormBwd {
 
 template <class XT, int V, bool EIGHT, bool NEED_F, bool PRE> struct BwdRing {
     // a stage: what is read of dx', dh, x^ (or x'), f^ (or f)
-    static constexpr int kX = sizeof(XT) * 8, kRow = kBwdThreads * V;
+    static constexpr int N = bwd_threads(V), kX = sizeof(XT) * 8, kRow = N * V;
     static constexpr int kDh = kX * kRow;
     static constexpr int kXh = kDh + (PRE ? 16 * kRow : 0);
     static constexpr int kFh = kXh + (PRE ? (EIGHT ? 8 : kX) * kRow : 0);
@@ -43,10 +43,10 @@ template <class XT, int V, bool EIGHT, bool NEED_F, bool PRE> struct BwdRing {
     static constexpr int kSums = 6 * 4 * 8 * kRow;       // at the end: up to six sums per column for each warp (team)
     static constexpr int kBytes = kDepth * kStage + kW + kG > kSums ? kDepth * kStage + kW + kG : kSums;
 };
-__device__ __forceinline__ void sts8(uint32_t slot, const f2 (&v)[4])
+template <int N> __device__ __forceinline__ void sts8(uint32_t slot, const f2 (&v)[4])
 {
     asm volatile("st.shared.v2.u64 [%0], {%1, %2};" ::"r"(slot), "l"(v[0]), "l"(v[1]) : "memory");
-    asm volatile("st.shared.v2.u64 [%0], {%1, %2};" ::"r"(slot + kBwdThreads * 16), "l"(v[2]), "l"(v[3]) : "memory");
+    asm volatile("st.shared.v2.u64 [%0], {%1, %2};" ::"r"(slot + N * 16), "l"(v[2]), "l"(v[3]) : "memory");
 }
 
 // Each team takes a run of consecutive rows and keeps the sums over them of its lanes' columns in registers: of dh x^ and dh for N_pre's
@@ -54,16 +54,16 @@ __device__ __forceinline__ void sts8(uint32_t slot, const f2 (&v)[4])
 //     dg = s (w1 B + b1 A),   dw1 = s sum_g g B_g,   db1 = s sum_g g A_g,      B = sum t f^,  A = sum t.
 // They go to memory once per block, A and B of several gates once per block and gate; k_norm_bwd_finish adds them up. 
 template <class XT, int L, int V, bool FULL, bool EIGHT, bool NEED_F, bool POST, bool PRE>
-__global__ void __launch_bounds__(kBwdThreads, 1) k_norm_bwd(const __grid_constant__ NormBwd p)
+__global__ void __launch_bounds__(bwd_threads(V), 1) k_norm_bwd(const __grid_constant__ NormBwd p)
 {
     using Ring = BwdRing<XT, V, EIGHT, NEED_F, PRE>;
-    constexpr int N = kBwdThreads, S = Ring::kDepth;
-    __shared__ float4 s_sum[2 * 8];
+    constexpr int N = Ring::N, S = Ring::kDepth;
+    __shared__ float4 s_sum[2 * (N / 32)];
     extern __shared__ __align__(128) uint8_t s_ring[];
     pdl_launch_dependents();
     Team<L> t(p.warps, V, s_sum);
     const int64_t team = (int64_t)blockIdx.x * p.teams + t.id;
-    const int64_t first = min(team * p.rows_per_team, p.rows), end = min(first + p.rows_per_team, p.rows);
+    const int64_t first = t.id < p.teams ? min(team * p.rows_per_team, p.rows) : p.rows, end = min(first + p.rows_per_team, p.rows);
     const int have = FULL ? V : max(0, min(V, (p.nvec - t.first_vec + L - 1) / L));
     const float inv = 1.0f / (float)p.cols;
     const uint32_t base = (uint32_t)__cvta_generic_to_shared(s_ring);
@@ -76,15 +76,15 @@ __global__ void __launch_bounds__(kBwdThreads, 1) k_norm_bwd(const __grid_consta
             for (int i = 0; i < V; i++)
                 if (i < have) {
                     const int c = (i * L + t.first_vec) * 8;
-                    if (p.dxo) async_row8<XT, N>(stage + at16 + i * kSlots<XT> * kBwdThreads * 16, static_cast<const XT *>(p.dxo) + row * p.lddxo + c);
+                    if (p.dxo) async_row8<XT, N>(stage + at16 + i * kSlots<XT> * N * 16, static_cast<const XT *>(p.dxo) + row * p.lddxo + c);
                     if (PRE) {
-                        async_row8<__nv_bfloat16, N>(stage + Ring::kDh + at16 + i * kBwdThreads * 16, p.dh + row * p.lddh + c);
-                        if (EIGHT) async8(stage + Ring::kXh + at8 + i * kBwdThreads * 8, p.xcodes + row * p.cols + c);
-                        else async_row8<XT, N>(stage + Ring::kXh + at16 + i * kSlots<XT> * kBwdThreads * 16, static_cast<const XT *>(p.xo) + row * p.ldxo + c);
+                        async_row8<__nv_bfloat16, N>(stage + Ring::kDh + at16 + i * N * 16, p.dh + row * p.lddh + c);
+                        if (EIGHT) async8(stage + Ring::kXh + at8 + i * N * 8, p.xcodes + row * p.cols + c);
+                        else async_row8<XT, N>(stage + Ring::kXh + at16 + i * kSlots<XT> * N * 16, static_cast<const XT *>(p.xo) + row * p.ldxo + c);
                     }
                     if (NEED_F) {
-                        if (EIGHT) async8(stage + Ring::kFh + at8 + i * kBwdThreads * 8, p.fcodes + row * p.cols + c);
-                        else async_row8<__nv_bfloat16, N>(stage + Ring::kFh + at16 + i * kBwdThreads * 16, p.f + row * p.ldf + c);
+                        if (EIGHT) async8(stage + Ring::kFh + at8 + i * N * 8, p.fcodes + row * p.cols + c);
+                        else async_row8<__nv_bfloat16, N>(stage + Ring::kFh + at16 + i * N * 16, p.f + row * p.ldf + c);
                     }
                 }
         }
@@ -123,7 +123,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) k_norm_bwd(const __grid_consta
             f2 w[4], none[4];
             zero8(w);
             if (i < have) load_side8({p.pre.w, nullptr, p.pre.fp32, 0, 0.0f}, i * L + t.first_vec, w, none);
-            sts8(w_at + i * kBwdThreads * 32, w);
+            sts8<N>(w_at + i * N * 32, w);
         }
     }
     const auto new_gate = [&](int64_t gate) {
@@ -140,7 +140,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) k_norm_bwd(const __grid_consta
 #pragma unroll
                 for (int j = 0; j < 4; j++) w[j] = f2_mul(w[j], f2_mul(g[j], f2_of(p.s, p.s)));
             }
-            sts8(g_at + i * kBwdThreads * 32, w);
+            sts8<N>(g_at + i * N * 32, w);
         }
     };
 
@@ -191,11 +191,11 @@ __global__ void __launch_bounds__(kBwdThreads, 1) k_norm_bwd(const __grid_consta
         for (int i = 0; i < V; i++) {
             if (PRE) {
                 if (FULL || i < n) {
-                    ring_row8<__nv_bfloat16, N>(stage + Ring::kDh + at16 + i * kBwdThreads * 16, d[i]);
+                    ring_row8<__nv_bfloat16, N>(stage + Ring::kDh + at16 + i * N * 16, d[i]);
                     if (EIGHT) {
-                        e4m3_to8(lds8(stage + Ring::kXh + at8 + i * kBwdThreads * 8), xsc[i], xh[i]);
+                        e4m3_to8(lds8(stage + Ring::kXh + at8 + i * N * 8), xsc[i], xh[i]);
                     } else {
-                        ring_row8<XT, N>(stage + Ring::kXh + at16 + i * kSlots<XT> * kBwdThreads * 16, xh[i]);
+                        ring_row8<XT, N>(stage + Ring::kXh + at16 + i * kSlots<XT> * N * 16, xh[i]);
                         const f2 m2 = f2_of(-pm0, -pm0), r2 = f2_of(pr0, pr0);
 #pragma unroll
                         for (int j = 0; j < 4; j++) xh[i][j] = f2_mul(f2_add(xh[i][j], m2), r2);
@@ -215,7 +215,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) k_norm_bwd(const __grid_consta
 #pragma unroll
             for (int i = 0; i < V; i++) {
                 f2 w[4];
-                ring_row8<float, N>(w_at + i * kBwdThreads * 32, w);
+                ring_row8<float, N>(w_at + i * N * 32, w);
                 c1[i] = c2[i] = 0;
 #pragma unroll
                 for (int j = 0; j < 4; j++) {
@@ -308,7 +308,8 @@ __global__ void __launch_bounds__(kBwdThreads, 1) k_norm_bwd(const __grid_consta
     // the block's sums: teams of one warp by shuffles, then each warp's (team's) sums side by side in shared memory
     async_wait<0>();
     __syncthreads();
-    const int wide = p.warps * 32, parts = kBwdThreads / wide, cols = p.cols;
+    const int wide = p.warps * 32, parts = L < 32 ? N / 32 : p.teams, cols = p.cols;
+    const bool in_team = L < 32 || t.id < p.teams;
     float *const mine = reinterpret_cast<float *>(s_ring) + (int64_t)(threadIdx.x / wide) * 4 * cols;
     const auto leave = [&](f2 (&v)[V][4], int which) {
 #pragma unroll
@@ -317,7 +318,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) k_norm_bwd(const __grid_consta
             for (int o = L; o < 32; o <<= 1)
 #pragma unroll
                 for (int j = 0; j < 4; j++) v[i][j] = f2_add(v[i][j], __shfl_xor_sync(0xFFFFFFFFu, v[i][j], o));
-            if (i < have && (threadIdx.x & 31) < L) store8(mine + which * cols + (i * L + t.first_vec) * 8, v[i]);
+            if (i < have && (threadIdx.x & 31) < L && in_team) store8(mine + which * cols + (i * L + t.first_vec) * 8, v[i]);
         }
     };
     const bool with_f = NEED_F && !p.several;
@@ -327,7 +328,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) k_norm_bwd(const __grid_consta
     if (NEED_F && p.several) {
 #pragma unroll
         for (int i = 0; i < V; i++)
-            if (FULL || i < have) {
+            if ((FULL || i < have) && in_team) {
                 float *o = last + (int64_t)t.id * 2 * cols + (i * L + t.first_vec) * 8;
                 store8(o, B[i]);
                 store8(o + cols, A[i]);
@@ -335,7 +336,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) k_norm_bwd(const __grid_consta
     }
     __syncthreads();
     float *part = p.part + (int64_t)blockIdx.x * 4 * cols;
-    for (int c = threadIdx.x * 4; c < 4 * cols; c += kBwdThreads * 4) {
+    for (int c = threadIdx.x * 4; c < 4 * cols; c += N * 4) {
         if (c < 2 * cols ? !PRE : !with_f) continue;
         float4 v = make_float4(0, 0, 0, 0);
         for (int k = 0; k < parts; k++) {
@@ -347,7 +348,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) k_norm_bwd(const __grid_consta
     if (NEED_F && p.several) {
         // along the block's teams: what they have of one gate follows each other, a team's first gate, (gates that are its own,) its last
         const int64_t row0 = (int64_t)blockIdx.x * p.teams * p.rows_per_team;
-        for (int c = threadIdx.x * 4; c < 2 * cols; c += kBwdThreads * 4) {
+        for (int c = threadIdx.x * 4; c < 2 * cols; c += N * 4) {
             float4 v = make_float4(0, 0, 0, 0);
             uint32_t now = (uint32_t)row0 / p.rows_per_gate;
             const auto add = [&](const float *at) {
@@ -375,12 +376,12 @@ __global__ void __launch_bounds__(kBwdThreads, 1) k_norm_bwd(const __grid_consta
 // Launches the kernel for rows of type XT and x^, f^ from checkpoints (EIGHT) or made again.
 template <class XT, bool EIGHT> cudaError_t launch_norm_bwd(const NormBwd &p, const RowPlan &plan, bool need_f, bool post, bool pre, cudaStream_t st)
 {
-    return with_lanes(plan, [&](auto l, auto v, auto full) {
+    return with_lanes<false>(plan, [&](auto l, auto v, auto full) {
         constexpr int L = decltype(l)::value, V = decltype(v)::value;
         return with_bools(need_f, post, pre, [&](auto f, auto q, auto r) -> cudaError_t {
             constexpr bool F = decltype(f)::value, Q = decltype(q)::value, R = decltype(r)::value;
             if constexpr ((Q && !F) || (!R && !F && EIGHT)) return cudaErrorInvalidValue;     // does not occur
-            else return launch_ring<k_norm_bwd<XT, L, V, decltype(full)::value, EIGHT, F, Q, R>, kBwdThreads>(plan.blocks, BwdRing<XT, V, EIGHT, F, R>::kBytes, st, p);
+            else return launch_ring<k_norm_bwd<XT, L, V, decltype(full)::value, EIGHT, F, Q, R>, bwd_threads(V)>(plan.blocks, BwdRing<XT, V, EIGHT, F, R>::kBytes, st, p);
         });
     });
 }

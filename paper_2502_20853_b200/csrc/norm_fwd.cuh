@@ -108,18 +108,6 @@ template <class XT, int V, bool HAS_F> struct FwdRing {
     static constexpr int kStage = kF + (HAS_F ? V * N * 16 : 0);
 };
 
-// A parameter of all columns in shared memory: two planes, the first and the second four of every eight columns.
-__device__ __forceinline__ void plane_put(float4 *plane, int nvec, int vec, const f2 (&v)[4])
-{
-    *reinterpret_cast<ulonglong2 *>(plane + vec) = make_ulonglong2(v[0], v[1]);
-    *reinterpret_cast<ulonglong2 *>(plane + nvec + vec) = make_ulonglong2(v[2], v[3]);
-}
-__device__ __forceinline__ void plane_get(const float4 *plane, int nvec, int vec, f2 (&v)[4])
-{
-    const ulonglong2 a = *reinterpret_cast<const ulonglong2 *>(plane + vec), b = *reinterpret_cast<const ulonglong2 *>(plane + nvec + vec);
-    v[0] = a.x, v[1] = a.y, v[2] = b.x, v[3] = b.y;
-}
-
 // x' = a x + (f^ cw + cb) [g], h = x^ pw + pb; cw = s w1 and cb = s b1, with one gate s g w1 and s g b1: the block keeps them in shared
 // memory as far as there are any (in registers they would leave room for eight warps instead of sixteen).
 template <class XT, int L, int V, bool FULL, bool HAS_F, bool POST, bool PRE>
@@ -132,7 +120,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) k_norm_fwd(const __grid_consta
     pdl_launch_dependents();
     Team<L> t(p.warps, V, s_sum);
     const int64_t team = (int64_t)blockIdx.x * p.teams + t.id;
-    const int64_t first = min(team * p.rows_per_team, p.rows), end = min(first + p.rows_per_team, p.rows);
+    const int64_t first = t.id < p.teams ? min(team * p.rows_per_team, p.rows) : p.rows, end = min(first + p.rows_per_team, p.rows);
     const int have = FULL ? V : max(0, min(V, (p.nvec - t.first_vec + L - 1) / L));   // vectors of this lane
     const float inv = 1.0f / (float)p.cols;
     const int S = p.stages;
@@ -339,7 +327,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) k_norm_fwd(const __grid_consta
 // Launches the kernel for rows of type XT.
 template <class XT> cudaError_t launch_norm_fwd(NormFwd &p, const RowPlan &plan, bool has_f, bool post, bool pre, cudaStream_t st)
 {
-    return with_lanes(plan, [&](auto l, auto v, auto full) {
+    return with_lanes<true>(plan, [&](auto l, auto v, auto full) {
         constexpr int L = decltype(l)::value, V = decltype(v)::value;
         return with_bools(has_f, post, pre, [&](auto f, auto q, auto r) -> cudaError_t {
             constexpr bool F = decltype(f)::value, Q = decltype(q)::value, R = decltype(r)::value;
