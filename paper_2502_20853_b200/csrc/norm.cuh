@@ -18,8 +18,9 @@ namespace mx {
 
 constexpr int kNormMaxCols = 8192;
 constexpr int kFwdThreads = 512;
-// Backward, by the vectors of a lane (their sums take 32 registers each): twelve warps with two, eight with three or four.
-constexpr int bwd_threads(int v) { return v == 2 ? 384 : 256; }
+// Backward: as many warps as the registers allow for v vectors of a lane and `sums` sums over rows (8 v registers each).  A kernel that
+// spills is twice as slow (50432 x 768: 80 us with eight warps, 158 with twelve and 200 bytes of spills): the ring leaves no L1 for them.
+constexpr int bwd_threads(int v, int sums) { return v == 2 ? (sums == 2 ? 512 : 384) : v == 3 && sums == 2 ? 384 : 256; }
 
 // ---- a lane's ring of rows in shared memory ----------------------------------------------------
 __device__ __forceinline__ void async16(uint32_t dst, const void *src) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory"); }
@@ -162,19 +163,20 @@ struct RowPlan {
 
     int warps() const { return lanes <= 32 ? 1 : lanes / 32; }
 };
-// Of v to 4 vectors per lane, and the fewest lanes that hold a row then, whatever leaves the fewest of a block's vectors without work; of
-// several the shorter lanes backward (more warps), the longer ones forward (fewer shuffles).
-template <bool FWD> inline RowPlan row_plan(int64_t rows, int64_t cols)
+// Of 3 or 4 vectors per lane, and the fewest lanes that hold a row then, whatever leaves the fewest of a block's vectors without work; of both
+// 4 (fewer shuffles).  Backward (sums > 0) 2, 3 where that fills the lanes, or 4 where a block of shorter lanes would be one team.
+inline RowPlan row_plan(int64_t rows, int64_t cols, int sums)
 {
     RowPlan b = {};
     const int64_t nvec = cols / 8;
     int best = 0;
-    for (int k = FWD ? 3 : 2; k <= 4; k++) {
-        const int threads = FWD ? kFwdThreads : bwd_threads(k);
-        int lanes = 4;
+    for (int k = sums ? 2 : 3; k <= 4; k++) {
+        const int threads = sums ? bwd_threads(k, sums) : kFwdThreads;
+        int lanes = sums && k == 4 ? 32 : 4;
         while (lanes * k < nvec) lanes += lanes < 32 ? lanes : 32;
+        if (sums && k == 3 && lanes * k != nvec) continue;
         const int teams = threads / lanes, used = (int)(teams * nvec * 1000 / (threads * k));     // in thousandths
-        if (teams > 0 && (FWD ? used >= best : used > best)) b.v = k, b.lanes = lanes, b.teams = teams, best = used;
+        if (teams > 0 && (sums ? used > best : used >= best)) b.v = k, b.lanes = lanes, b.teams = teams, best = used;
     }
     b.full = (int64_t)b.v * b.lanes * 8 == cols;
     const int64_t teams = b.teams, most = ceil_div(rows, teams);
@@ -239,21 +241,14 @@ template <auto KERNEL, int THREADS, class P> inline cudaError_t launch_ring(int 
     const cudaError_t e = set_smem_once(attr_set, KERNEL, kRingBytes);
     return e != cudaSuccess ? e : launch_pdl(KERNEL, (unsigned)blocks, 1, THREADS, smem, st, p);
 }
-template <int V, class F> inline cudaError_t with_lanes_of(const RowPlan &plan, F &&f)
+template <int V, class F> inline cudaError_t with_lanes(const RowPlan &plan, F &&f)     // f(lanes of a warp's part of a team, full)
 {
     return with_bools(plan.full, false, false, [&](auto full, auto, auto) {
-        const std::integral_constant<int, V> v;
-        return plan.lanes == 4    ? f(std::integral_constant<int, 4>(), v, full)
-               : plan.lanes == 8  ? f(std::integral_constant<int, 8>(), v, full)
-               : plan.lanes == 16 ? f(std::integral_constant<int, 16>(), v, full)
-                                  : f(std::integral_constant<int, 32>(), v, full);
+        return plan.lanes == 4    ? f(std::integral_constant<int, 4>(), full)
+               : plan.lanes == 8  ? f(std::integral_constant<int, 8>(), full)
+               : plan.lanes == 16 ? f(std::integral_constant<int, 16>(), full)
+                                  : f(std::integral_constant<int, 32>(), full);
     });
-}
-template <bool FWD, class F> inline cudaError_t with_lanes(const RowPlan &plan, F &&f)     // f(lanes of a warp's part of a team, vectors, full)
-{
-    if constexpr (!FWD)
-        if (plan.v == 2) return with_lanes_of<2>(plan, f);
-    return plan.v == 3 ? with_lanes_of<3>(plan, f) : with_lanes_of<4>(plan, f);
 }
 
 }  // namespace mx

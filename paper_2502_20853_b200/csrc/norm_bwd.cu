@@ -1,13 +1,15 @@
 // Residual addition between two norms, backward: the entry points, the reduction of what the blocks leave, and the kernel for rows of bf16
 // with checkpoints.
+#include <algorithm>
+
 #include "norm_bwd.cuh"
 
 namespace mx {
 
-template cudaError_t launch_norm_bwd<__nv_bfloat16, true>(const NormBwd &, const RowPlan &, bool, bool, bool, cudaStream_t);
-extern template cudaError_t launch_norm_bwd<__nv_bfloat16, false>(const NormBwd &, const RowPlan &, bool, bool, bool, cudaStream_t);
-extern template cudaError_t launch_norm_bwd<float, true>(const NormBwd &, const RowPlan &, bool, bool, bool, cudaStream_t);
-extern template cudaError_t launch_norm_bwd<float, false>(const NormBwd &, const RowPlan &, bool, bool, bool, cudaStream_t);
+template cudaError_t launch_norm_bwd<__nv_bfloat16, true>(const NormBwd &, const RowPlan &, bool, bool, bool, bool, bool, cudaStream_t);
+extern template cudaError_t launch_norm_bwd<__nv_bfloat16, false>(const NormBwd &, const RowPlan &, bool, bool, bool, bool, bool, cudaStream_t);
+extern template cudaError_t launch_norm_bwd<float, true>(const NormBwd &, const RowPlan &, bool, bool, bool, bool, bool, cudaStream_t);
+extern template cudaError_t launch_norm_bwd<float, false>(const NormBwd &, const RowPlan &, bool, bool, bool, bool, bool, cudaStream_t);
 
 struct NormBwdFinish {
     const float *part, *slots;
@@ -16,7 +18,7 @@ struct NormBwdFinish {
     int64_t ldg, gates;
     int gate_fp32, several;
     float s;
-    int blocks, pre, use_f, has_post;
+    int blocks, pre, use_f, has_post, sb, sa;
     int64_t rows, rows_per_gate, rows_per_block;
     int cols, slices;         // slices of 128 columns
     float *dw_pre, *db_pre, *dw_post, *db_post, *dgate;
@@ -56,8 +58,10 @@ __global__ void __launch_bounds__(256) k_norm_bwd_finish(const __grid_constant__
         const bool f = p.use_f && !p.several;
         for (int k = r; k < p.blocks; k += 64) {
             const float *at = p.part + (int64_t)k * 4 * p.cols + c;
-            if (p.pre) add4(v[0], load4(at)), add4(v[1], load4(at + p.cols));
-            if (f) add4(v[2], load4(at + 2 * p.cols)), add4(v[3], load4(at + 3 * p.cols));
+            if (p.pre) add4(v[0], load4(at));
+            if (p.sb) add4(v[1], load4(at + p.cols));
+            if (f) add4(v[2], load4(at + 2 * p.cols));
+            if (f && p.sa) add4(v[3], load4(at + 3 * p.cols));
         }
         if (p.use_f && p.several && (p.dw_post || p.db_post))
             for (int k = r; k < p.blocks; k += 64) {
@@ -118,8 +122,12 @@ extern "C" {
 size_t mxfp4_residual_norm_workspace_bytes(int64_t rows, int64_t cols, int64_t gates)
 {
     if (rows <= 0 || cols <= 0 || cols > kNormMaxCols || gates < 0) return 0;
-    const RowPlan b = row_plan<false>(rows, cols);
-    return (size_t)(part_floats(b, cols) + slot_floats(b, cols, gates)) * 4;
+    int64_t most = 0;      // whichever gradients are asked for
+    for (int sums = 2; sums <= 4; sums++) {
+        const RowPlan b = row_plan(rows, cols, sums);
+        most = std::max(most, part_floats(b, cols) + slot_floats(b, cols, gates));
+    }
+    return (size_t)most * 4;
 }
 
 mxfp4_status_t mxfp4_residual_norm_bwd(const mxfp4_residual_norm_t *n, const mxfp4_residual_norm_bwd_t *b, void *workspace, size_t workspace_bytes, void *stream)
@@ -155,8 +163,9 @@ mxfp4_status_t mxfp4_residual_norm_bwd(const mxfp4_residual_norm_t *n, const mxf
     if (need_f && !eight && (s = check_rows(b->f_bf16, b->ldf, cols, MXFP4_OUT_BF16))) return s;
     if (!workspace) return MXFP4_INVALID_ARG;
     if (reinterpret_cast<uintptr_t>(workspace) & 255u) return MXFP4_MISALIGNED;
-    const RowPlan plan = row_plan<false>(rows, cols);
-    if (workspace_bytes < (size_t)(part_floats(plan, cols) + slot_floats(plan, cols, n->gates)) * 4) return MXFP4_WORKSPACE_TOO_SMALL;
+    const bool sb = b->db_pre, sa = post && (b->db_post || (b->dgate && n->post.bias));
+    const RowPlan plan = row_plan(rows, cols, 2 + sb + sa);
+    if (workspace_bytes < mxfp4_residual_norm_workspace_bytes(rows, cols, n->gates)) return MXFP4_WORKSPACE_TOO_SMALL;
     {
         // dx and df are written row by row while later rows are still to be read
         const Span dx = span_of_rows(b->dx, b->lddx, rows, cols, xb), df = span_of_rows(b->df_bf16, b->lddf, rows, cols, 2);
@@ -183,11 +192,11 @@ mxfp4_status_t mxfp4_residual_norm_bwd(const mxfp4_residual_norm_t *n, const mxf
     p.rows = rows, p.rows_per_team = plan.rows_per_team, p.cols = (int)cols, p.nvec = (int)(cols / 8), p.warps = plan.warps(), p.teams = plan.teams;
     const auto go = n->x_dtype == MXFP4_OUT_FP32 ? (eight ? launch_norm_bwd<float, true> : launch_norm_bwd<float, false>)
                                                  : (eight ? launch_norm_bwd<__nv_bfloat16, true> : launch_norm_bwd<__nv_bfloat16, false>);
-    MX_CHECK_CUDA(go(p, plan, need_f, post, pre, st));
+    MX_CHECK_CUDA(go(p, plan, need_f, post, pre, sb, sa, st));
     if (!b->dw_pre && !b->db_pre && !b->dw_post && !b->db_post && !b->dgate) return MXFP4_OK;
     NormBwdFinish e = {};
     e.part = p.part, e.slots = p.slots, e.post = p.post, e.gate = p.gate, e.ldg = p.ldg, e.gate_fp32 = p.gate_fp32;
-    e.gates = n->gates > 1 ? n->gates : 1, e.several = p.several, e.s = p.s, e.blocks = plan.blocks, e.pre = pre, e.use_f = need_f, e.has_post = post;
+    e.gates = n->gates > 1 ? n->gates : 1, e.several = p.several, e.s = p.s, e.blocks = plan.blocks, e.pre = pre, e.use_f = need_f, e.has_post = post, e.sb = sb, e.sa = sa;
     e.rows = rows, e.rows_per_gate = p.rows_per_gate, e.rows_per_block = plan.rows_per_team * plan.teams, e.cols = (int)cols;
     e.slices = (int)ceil_div(cols, 128);
     e.dw_pre = b->dw_pre, e.db_pre = b->db_pre, e.dw_post = b->dw_post, e.db_post = b->db_post, e.dgate = b->dgate;

@@ -30,9 +30,9 @@ struct NormBwd {
     int cols, nvec, warps, teams;     // of a team; of a block
 };
 
-template <class XT, int V, bool EIGHT, bool NEED_F, bool PRE> struct BwdRing {
+template <class XT, int V, int SUMS, bool EIGHT, bool NEED_F, bool PRE> struct BwdRing {
     // a stage: what is read of dx', dh, x^ (or x'), f^ (or f)
-    static constexpr int N = bwd_threads(V), kX = sizeof(XT) * 8, kRow = N * V;
+    static constexpr int N = bwd_threads(V, SUMS), kX = sizeof(XT) * 8, kRow = N * V;
     static constexpr int kDh = kX * kRow;
     static constexpr int kXh = kDh + (PRE ? 16 * kRow : 0);
     static constexpr int kFh = kXh + (PRE ? (EIGHT ? 8 : kX) * kRow : 0);
@@ -53,10 +53,11 @@ template <int N> __device__ __forceinline__ void sts8(uint32_t slot, const f2 (&
 // gradients, and of t f^ and t (t the gradient of x' in all) for those of N_post and the gate:  with g constant over the rows of a gate,
 //     dg = s (w1 B + b1 A),   dw1 = s sum_g g B_g,   db1 = s sum_g g A_g,      B = sum t f^,  A = sum t.
 // They go to memory once per block, A and B of several gates once per block and gate; k_norm_bwd_finish adds them up. 
-template <class XT, int L, int V, bool FULL, bool EIGHT, bool NEED_F, bool POST, bool PRE>
-__global__ void __launch_bounds__(bwd_threads(V), 1) k_norm_bwd(const __grid_constant__ NormBwd p)
+// SB, SA: the sums of dh and of t are wanted.
+template <class XT, int L, int V, bool FULL, bool EIGHT, bool NEED_F, bool POST, bool PRE, bool SB, bool SA>
+__global__ void __launch_bounds__(bwd_threads(V, 2 + SB + SA), 1) k_norm_bwd(const __grid_constant__ NormBwd p)
 {
-    using Ring = BwdRing<XT, V, EIGHT, NEED_F, PRE>;
+    using Ring = BwdRing<XT, V, 2 + SB + SA, EIGHT, NEED_F, PRE>;
     constexpr int N = Ring::N, S = Ring::kDepth;
     __shared__ float4 s_sum[2 * (N / 32)];
     extern __shared__ __align__(128) uint8_t s_ring[];
@@ -220,7 +221,7 @@ __global__ void __launch_bounds__(bwd_threads(V), 1) k_norm_bwd(const __grid_con
 #pragma unroll
                 for (int j = 0; j < 4; j++) {
                     sw[i][j] = f2_fma(d[i][j], xh[i][j], sw[i][j]);
-                    sb[i][j] = f2_add(d[i][j], sb[i][j]);
+                    if (SB) sb[i][j] = f2_add(d[i][j], sb[i][j]);
                     d[i][j] = f2_mul(d[i][j], w[j]);
                     c1[i] = j ? f2_add(c1[i], d[i][j]) : d[i][j];
                     c2[i] = j ? f2_fma(d[i][j], xh[i][j], c2[i]) : f2_mul(d[i][j], xh[i][j]);
@@ -271,7 +272,7 @@ __global__ void __launch_bounds__(bwd_threads(V), 1) k_norm_bwd(const __grid_con
 #pragma unroll
                 for (int j = 0; j < 4; j++) {
                     B[i][j] = f2_fma(x[j], xh[i][j], B[i][j]);
-                    A[i][j] = f2_add(x[j], A[i][j]);
+                    if (SA) A[i][j] = f2_add(x[j], A[i][j]);
                     d[i][j] = f2_mul(x[j], w[j]);
                     if (POST) {
                         e1[i] = j ? f2_add(e1[i], d[i][j]) : d[i][j];
@@ -322,8 +323,10 @@ __global__ void __launch_bounds__(bwd_threads(V), 1) k_norm_bwd(const __grid_con
         }
     };
     const bool with_f = NEED_F && !p.several;
-    if (PRE) leave(sw, 0), leave(sb, 1);
-    if (with_f) leave(B, 2), leave(A, 3);
+    if (PRE) leave(sw, 0);
+    if (PRE && SB) leave(sb, 1);
+    if (with_f) leave(B, 2);
+    if (with_f && SA) leave(A, 3);
     float *const last = reinterpret_cast<float *>(s_ring) + (int64_t)parts * 4 * cols;     // [team][2][cols]: of each team's last gate
     if (NEED_F && p.several) {
 #pragma unroll
@@ -337,7 +340,8 @@ __global__ void __launch_bounds__(bwd_threads(V), 1) k_norm_bwd(const __grid_con
     __syncthreads();
     float *part = p.part + (int64_t)blockIdx.x * 4 * cols;
     for (int c = threadIdx.x * 4; c < 4 * cols; c += N * 4) {
-        if (c < 2 * cols ? !PRE : !with_f) continue;
+        const int which = c / cols;
+        if (which < 2 ? !PRE || (which == 1 && !SB) : !with_f || (which == 3 && !SA)) continue;
         float4 v = make_float4(0, 0, 0, 0);
         for (int k = 0; k < parts; k++) {
             const float4 w = reinterpret_cast<const float4 *>(s_ring)[k * cols + c / 4];
@@ -373,17 +377,33 @@ __global__ void __launch_bounds__(bwd_threads(V), 1) k_norm_bwd(const __grid_con
     }
 }
 
-// Launches the kernel for rows of type XT and x^, f^ from checkpoints (EIGHT) or made again.
-template <class XT, bool EIGHT> cudaError_t launch_norm_bwd(const NormBwd &p, const RowPlan &plan, bool need_f, bool post, bool pre, cudaStream_t st)
+// Launches the kernel for rows of type XT and x^, f^ from checkpoints (EIGHT) or made again.  `sb`, `sa`: whether the sums of dh and of t are wanted.
+template <class XT, bool EIGHT> cudaError_t launch_norm_bwd(const NormBwd &p, const RowPlan &plan, bool need_f, bool post, bool pre, bool sb, bool sa, cudaStream_t st)
 {
-    return with_lanes<false>(plan, [&](auto l, auto v, auto full) {
+    const auto go = [&](auto l, auto v, auto full) {
         constexpr int L = decltype(l)::value, V = decltype(v)::value;
         return with_bools(need_f, post, pre, [&](auto f, auto q, auto r) -> cudaError_t {
             constexpr bool F = decltype(f)::value, Q = decltype(q)::value, R = decltype(r)::value;
-            if constexpr ((Q && !F) || (!R && !F && EIGHT)) return cudaErrorInvalidValue;     // does not occur
-            else return launch_ring<k_norm_bwd<XT, L, V, decltype(full)::value, EIGHT, F, Q, R>, bwd_threads(V)>(plan.blocks, BwdRing<XT, V, EIGHT, F, R>::kBytes, st, p);
+            if constexpr ((Q && !F) || (!R && !F && EIGHT)) {
+                return cudaErrorInvalidValue;     // does not occur
+            } else {
+                return with_bools(sb, sa, false, [&](auto b, auto a, auto) -> cudaError_t {
+                    constexpr bool B = decltype(b)::value, A = decltype(a)::value;
+                    if constexpr ((B && !R) || (A && !Q)) return cudaErrorInvalidValue;     // does not occur
+                    else
+                        return launch_ring<k_norm_bwd<XT, L, V, decltype(full)::value, EIGHT, F, Q, R, B, A>, bwd_threads(V, 2 + B + A)>(
+                            plan.blocks, BwdRing<XT, V, 2 + B + A, EIGHT, F, R>::kBytes, st, p);
+                });
+            }
         });
-    });
+    };
+    using L32 = std::integral_constant<int, 32>;
+    const std::integral_constant<int, 2> two;
+    const std::integral_constant<int, 3> three;
+    const std::integral_constant<int, 4> four;
+    if (plan.v == 2) return with_lanes<2>(plan, [&](auto l, auto full) { return go(l, two, full); });
+    if (plan.v == 3) return with_lanes<3>(plan, [&](auto l, auto) { return go(l, three, std::true_type()); });
+    return plan.full ? go(L32(), four, std::true_type()) : go(L32(), four, std::false_type());
 }
 
 }  // namespace mx

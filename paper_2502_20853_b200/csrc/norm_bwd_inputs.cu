@@ -3,6 +3,6 @@
 
 namespace mx {
 
-template cudaError_t launch_norm_bwd<__nv_bfloat16, false>(const NormBwd &, const RowPlan &, bool, bool, bool, cudaStream_t);
+template cudaError_t launch_norm_bwd<__nv_bfloat16, false>(const NormBwd &, const RowPlan &, bool, bool, bool, bool, bool, cudaStream_t);
 
 }  // namespace mx

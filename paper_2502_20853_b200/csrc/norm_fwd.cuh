@@ -327,7 +327,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) k_norm_fwd(const __grid_consta
 // Launches the kernel for rows of type XT.
 template <class XT> cudaError_t launch_norm_fwd(NormFwd &p, const RowPlan &plan, bool has_f, bool post, bool pre, cudaStream_t st)
 {
-    return with_lanes<true>(plan, [&](auto l, auto v, auto full) {
+    const auto go = [&](auto l, auto v, auto full) {
         constexpr int L = decltype(l)::value, V = decltype(v)::value;
         return with_bools(has_f, post, pre, [&](auto f, auto q, auto r) -> cudaError_t {
             constexpr bool F = decltype(f)::value, Q = decltype(q)::value, R = decltype(r)::value;
@@ -339,7 +339,9 @@ template <class XT> cudaError_t launch_norm_fwd(NormFwd &p, const RowPlan &plan,
                 return launch_ring<k_norm_fwd<XT, L, V, decltype(full)::value, F, Q, R>, kFwdThreads>(plan.blocks, p.stages * FwdRing<XT, V, F>::kStage + planes, st, p);
             }
         });
-    });
+    };
+    if (plan.v == 3) return with_lanes<3>(plan, [&](auto l, auto full) { return go(l, std::integral_constant<int, 3>(), full); });
+    return with_lanes<4>(plan, [&](auto l, auto full) { return go(l, std::integral_constant<int, 4>(), full); });
 }
 
 }  // namespace mx
