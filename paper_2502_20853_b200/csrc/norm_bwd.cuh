@@ -65,35 +65,46 @@ __global__ void __launch_bounds__(bwd_threads(V, 2 + SB + SA), 1) k_norm_bwd(con
     Team<L> t(p.warps, V, s_sum);
     const int64_t team = (int64_t)blockIdx.x * p.teams + t.id;
     const int64_t first = t.id < p.teams ? min(team * p.rows_per_team, p.rows) : p.rows, end = min(first + p.rows_per_team, p.rows);
+    constexpr bool EXACT = FULL && L == 32;      // each turn of each lane has a row and all of its vectors
     const int have = FULL ? V : max(0, min(V, (p.nvec - t.first_vec + L - 1) / L));
     const float inv = 1.0f / (float)p.cols;
     const uint32_t base = (uint32_t)__cvta_generic_to_shared(s_ring);
     const uint32_t at16 = threadIdx.x * 16, at8 = threadIdx.x * 8;
     pdl_wait();
 
+    // the lane's places in the row that is fetched next
+    const XT *dxo_at = static_cast<const XT *>(p.dxo) + first * p.lddxo + t.first_vec * 8, *xo_at = static_cast<const XT *>(p.xo) + first * p.ldxo + t.first_vec * 8;
+    const __nv_bfloat16 *dh_at = p.dh + first * p.lddh + t.first_vec * 8, *f_at = p.f + first * p.ldf + t.first_vec * 8;
+    const uint8_t *xc_at = p.xcodes + first * p.cols + t.first_vec * 8, *fc_at = p.fcodes + first * p.cols + t.first_vec * 8;
     const auto fetch = [&](int64_t row, uint32_t stage) {
         if (row < end) {
 #pragma unroll
             for (int i = 0; i < V; i++)
-                if (i < have) {
-                    const int c = (i * L + t.first_vec) * 8;
-                    if (p.dxo) async_row8<XT, N>(stage + at16 + i * kSlots<XT> * N * 16, static_cast<const XT *>(p.dxo) + row * p.lddxo + c);
+                if (FULL || i < have) {
+                    if (p.dxo) async_row8<XT, N>(stage + at16 + i * kSlots<XT> * N * 16, dxo_at + i * L * 8);
                     if (PRE) {
-                        async_row8<__nv_bfloat16, N>(stage + Ring::kDh + at16 + i * N * 16, p.dh + row * p.lddh + c);
-                        if (EIGHT) async8(stage + Ring::kXh + at8 + i * N * 8, p.xcodes + row * p.cols + c);
-                        else async_row8<XT, N>(stage + Ring::kXh + at16 + i * kSlots<XT> * N * 16, static_cast<const XT *>(p.xo) + row * p.ldxo + c);
+                        async_row8<__nv_bfloat16, N>(stage + Ring::kDh + at16 + i * N * 16, dh_at + i * L * 8);
+                        if (EIGHT) async8(stage + Ring::kXh + at8 + i * N * 8, xc_at + i * L * 8);
+                        else async_row8<XT, N>(stage + Ring::kXh + at16 + i * kSlots<XT> * N * 16, xo_at + i * L * 8);
                     }
                     if (NEED_F) {
-                        if (EIGHT) async8(stage + Ring::kFh + at8 + i * N * 8, p.fcodes + row * p.cols + c);
-                        else async_row8<__nv_bfloat16, N>(stage + Ring::kFh + at16 + i * N * 16, p.f + row * p.ldf + c);
+                        if (EIGHT) async8(stage + Ring::kFh + at8 + i * N * 8, fc_at + i * L * 8);
+                        else async_row8<__nv_bfloat16, N>(stage + Ring::kFh + at16 + i * N * 16, f_at + i * L * 8);
                     }
                 }
+            dxo_at += p.lddxo;
+            if (PRE) dh_at += p.lddh;
+            if (PRE && EIGHT) xc_at += p.cols;
+            if (PRE && !EIGHT) xo_at += p.ldxo;
+            if (NEED_F && EIGHT) fc_at += p.cols;
+            if (NEED_F && !EIGHT) f_at += p.ldf;
         }
         async_commit();
     };
     // what is too small for the ring: statistics and scale bytes, one row ahead in registers
     float pm, pr, qm, qr;
     uint32_t xs[V], fs[V];
+    const uint8_t *xs_at = p.xscales + first * (p.cols >> 5) + (t.first_vec >> 2), *fs_at = p.fscales + first * (p.cols >> 5) + (t.first_vec >> 2);
     const auto fetch_small = [&](int64_t row) {
         if (row >= end) return;
         if (PRE) pr = p.stats[p.rows + row];
@@ -103,13 +114,19 @@ __global__ void __launch_bounds__(bwd_threads(V, 2 + SB + SA), 1) k_norm_bwd(con
         if (EIGHT) {
 #pragma unroll
             for (int i = 0; i < V; i++)
-                if (i < have) {
-                    const int64_t at = row * (p.cols >> 5) + ((i * L + t.first_vec) >> 2);
-                    if (PRE) xs[i] = p.xscales[at];
-                    if (NEED_F) fs[i] = p.fscales[at];
+                if (FULL || i < have) {
+                    if (PRE) xs[i] = xs_at[i * (L / 4)];
+                    if (NEED_F) fs[i] = fs_at[i * (L / 4)];
                 }
+            xs_at += p.cols >> 5, fs_at += p.cols >> 5;
         }
     };
+    if (!p.dxo) {       // nothing comes from further on: the slots stay zeros
+        for (int k = 0; k < S; k++)
+#pragma unroll
+            for (int i = 0; i < V * kSlots<XT>; i++)
+                asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(base + k * Ring::kStage + at16 + i * N * 16), "r"(0) : "memory");
+    }
 #pragma unroll
     for (int k = 0; k < S - 1; k++) fetch(first + k, base + k * Ring::kStage);
     pm = pr = qm = qr = 0.0f;
@@ -165,10 +182,12 @@ __global__ void __launch_bounds__(bwd_threads(V, 2 + SB + SA), 1) k_norm_bwd(con
     };
 
     uint32_t slot = 0;
+    XT *dx = static_cast<XT *>(p.dx) + first * p.lddx + t.first_vec * 8;       // the lane's places in this row
+    __nv_bfloat16 *df = p.df + first * p.lddf + t.first_vec * 8;
     const int turns = turns_of<L>((int)p.rows_per_team, first, end);
-    for (int k = 0; k < turns; k++) {
+    for (int k = 0; k < turns; k++, dx += p.lddx, df += p.lddf) {
         const int64_t row = first + k;
-        const bool live = row < end;
+        const bool live = EXACT || row < end;
         const int n = live ? have : 0;
         fetch(row + S - 1, base + (slot == 0 ? S - 1 : slot - 1) * Ring::kStage);
         const uint32_t stage = base + slot * Ring::kStage;
@@ -206,7 +225,7 @@ __global__ void __launch_bounds__(bwd_threads(V, 2 + SB + SA), 1) k_norm_bwd(con
                 }
             }
         }
-        if (FULL && PRE && !live) {       // what the ring holds for a row that is none: a lane of a team beside a longer one
+        if (FULL && !EXACT && PRE && !live) {       // what the ring holds for a row that is none: a lane of a team beside a longer one
 #pragma unroll
             for (int i = 0; i < V; i++) zero8(d[i]), zero8(xh[i]);
         }
@@ -233,24 +252,28 @@ __global__ void __launch_bounds__(bwd_threads(V, 2 + SB + SA), 1) k_norm_bwd(con
             team_sum(t, c);
         }
         const float m1 = p.pre.rms ? 0.0f : -c[0] * inv, m2 = -c[1] * inv;
-        const f2 k1 = f2_of(m1, m1), k2 = f2_of(m2, m2), kr = f2_of(pr0, pr0), ka = f2_of(p.a, p.a), ks = f2_of(p.s, p.s);
+        // t = dx' + r (d + m1 + m2 x^)
+        const f2 k1 = f2_of(m1 * pr0, m1 * pr0), k2 = f2_of(m2 * pr0, m2 * pr0), kr = f2_of(pr0, pr0);
         f2 e1[V], e2[V];
-        XT *const dx = static_cast<XT *>(p.dx) + row * p.lddx + t.first_vec * 8;
 #pragma unroll
         for (int i = 0; i < V; i++) {
             const bool on = FULL ? live : i < n;
             f2 x[4];
-            zero8(x);
-            if (p.dxo && on) ring_row8<XT, N>(stage + at16 + i * kSlots<XT> * N * 16, x);
+            if (on) ring_row8<XT, N>(stage + at16 + i * kSlots<XT> * N * 16, x);
+            else zero8(x);
             if (PRE && on) {
 #pragma unroll
-                for (int j = 0; j < 4; j++) x[j] = f2_fma(kr, f2_fma(xh[i][j], k2, f2_add(d[i][j], k1)), x[j]);
+                for (int j = 0; j < 4; j++) x[j] = f2_add(x[j], f2_fma(d[i][j], kr, f2_fma(xh[i][j], k2, k1)));
             }
             if (on) {
-                f2 y[4];
+                if (p.a == 1.0f) {
+                    store8(dx + i * L * 8, x);
+                } else {
+                    f2 y[4];
 #pragma unroll
-                for (int j = 0; j < 4; j++) y[j] = f2_mul(x[j], ka);
-                store8(dx + i * L * 8, y);
+                    for (int j = 0; j < 4; j++) y[j] = f2_mul(x[j], f2_of(p.a, p.a));
+                    store8(dx + i * L * 8, y);
+                }
             }
             // the branch: from here on xh is f^, and d the gradient of f^, then of f
             e1[i] = e2[i] = 0;
@@ -281,7 +304,7 @@ __global__ void __launch_bounds__(bwd_threads(V, 2 + SB + SA), 1) k_norm_bwd(con
                 }
             } else {
 #pragma unroll
-                for (int j = 0; j < 4; j++) d[i][j] = f2_mul(x[j], ks);
+                for (int j = 0; j < 4; j++) d[i][j] = f2_mul(x[j], f2_of(p.s, p.s));
             }
         }
         if (NEED_F) {
@@ -291,18 +314,17 @@ __global__ void __launch_bounds__(bwd_threads(V, 2 + SB + SA), 1) k_norm_bwd(con
                 float e[2] = {f2_sum(e1[0]), f2_sum(e2[0])};
                 team_sum(t, e);
                 const float n1 = p.post.rms ? 0.0f : -e[0] * inv, n2 = -e[1] * inv;
-                const f2 a1 = f2_of(n1, n1), a2 = f2_of(n2, n2), r2 = f2_of(qr0, qr0);
+                const f2 a1 = f2_of(n1 * qr0, n1 * qr0), a2 = f2_of(n2 * qr0, n2 * qr0), r2 = f2_of(qr0, qr0);
 #pragma unroll
                 for (int i = 0; i < V; i++)
 #pragma unroll
-                    for (int j = 0; j < 4; j++) d[i][j] = f2_mul(r2, f2_fma(xh[i][j], a2, f2_add(d[i][j], a1)));
+                    for (int j = 0; j < 4; j++) d[i][j] = f2_fma(d[i][j], r2, f2_fma(xh[i][j], a2, a1));
             }
         }
         if (p.df && live) {
-            __nv_bfloat16 *o = p.df + row * p.lddf;
 #pragma unroll
             for (int i = 0; i < V; i++)
-                if (FULL || i < n) store8(o + (i * L + t.first_vec) * 8, d[i]);
+                if (FULL || i < n) store8(df + i * L * 8, d[i]);
         }
     }
 
