@@ -28,7 +28,7 @@ struct NormFwd {
     uint32_t *dev_status;
 };
 
-// mean and 1 / sqrt(var + eps) of the row that the lanes hold (zeros behind its end), by two passes; then the row is normalized.
+// mean and 1 / sqrt(var + eps) of the row that the lanes hold (zeros behind its end), by two passes; the row is left without its mean.
 // `have`: vectors that this lane holds of the row (all, where it is FULL).
 template <int V, bool FULL, int L>
 __device__ __forceinline__ void normalize(Team<L> &t, const NormSide &n, float inv, int have, f2 (&v)[V][4], float &mean, float &rstd)
@@ -62,27 +62,22 @@ __device__ __forceinline__ void normalize(Team<L> &t, const NormSide &n, float i
     s[0] = f2_sum(acc[0]);
     team_sum(t, s);
     rstd = rsqrtf(s[0] * inv + n.eps);      // to 2^-23
-    const f2 r2 = f2_of(rstd, rstd);
-#pragma unroll
-    for (int i = 0; i < V; i++)
-#pragma unroll
-        for (int j = 0; j < 4; j++) v[i][j] = f2_mul(v[i][j], r2);
 }
 
-// The checkpoint of the row.  `n`: vectors of this lane that are written; `at`: where the lane's first one is, in eights of the matrix.
+// The checkpoint of the row v r.  `n`: vectors of this lane that are written; `at`: where the lane's first one is, in eights of the matrix.
 template <int V, bool FULL, int L>
-__device__ __forceinline__ bool row_ckpt(const CkptOut &o, const Team<L> &t, int n, const f2 (&v)[V][4], int64_t at)
+__device__ __forceinline__ bool row_ckpt(const CkptOut &o, const Team<L> &t, int n, const f2 (&v)[V][4], float r, int64_t at)
 {
     uint32_t m[V], byte[V], worst = 0;
     uint2 c[V];
 #pragma unroll
     for (int i = 0; i < V; i++) m[i] = amax8(v[i]);
 #pragma unroll
-    for (int i = 0; i < V; i++) m[i] = group_max4(m[i]);
+    for (int i = 0; i < V; i++) m[i] = __float_as_uint(__uint_as_float(group_max4(m[i])) * r);     // the largest |v r|: rounding keeps the order
 #pragma unroll
     for (int i = 0; i < V; i++) {
         byte[i] = ckpt_scale_byte(m[i], o.tf_add);
-        c[i] = e4m3_x8(v[i], __uint_as_float((254u - byte[i]) << 23));
+        c[i] = e4m3_x8(v[i], __uint_as_float((254u - byte[i]) << 23) * r);
         worst = max(worst, m[i]);
     }
     if (worst >= 0x7F800000u) {      // a group that is not finite: aside, it costs the others one comparison
@@ -121,6 +116,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) k_norm_fwd(const __grid_consta
     Team<L> t(p.warps, V, s_sum);
     const int64_t team = (int64_t)blockIdx.x * p.teams + t.id;
     const int64_t first = t.id < p.teams ? min(team * p.rows_per_team, p.rows) : p.rows, end = min(first + p.rows_per_team, p.rows);
+    constexpr bool EXACT = FULL && L == 32;      // each turn of each lane has a row and all of its vectors
     const int have = FULL ? V : max(0, min(V, (p.nvec - t.first_vec + L - 1) / L));   // vectors of this lane
     const float inv = 1.0f / (float)p.cols;
     const int S = p.stages;
@@ -182,7 +178,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) k_norm_fwd(const __grid_consta
     const int turns = turns_of<L>((int)p.rows_per_team, first, end);
     for (int k = 0; k < turns; k++) {
         const int64_t row = first + k;
-        const bool live = row < end;
+        const bool live = EXACT || row < end;
         fetch(row + S - 1, ring + (slot == 0 ? S - 1 : slot - 1) * Ring::kStage);
         const uint32_t stage = ring + slot * Ring::kStage;
         slot = slot == S - 1 ? 0 : slot + 1;
@@ -193,6 +189,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) k_norm_fwd(const __grid_consta
         const int n = live ? have : 0;
         async_wait_all_but(S - 1);
         f2 v[V][4];
+        float r = 1.0f;
         if (HAS_F) {
 #pragma unroll
             for (int i = 0; i < V; i++) {
@@ -200,11 +197,11 @@ __global__ void __launch_bounds__(kFwdThreads, 1) k_norm_fwd(const __grid_consta
                 else zero8(v[i]);
             }
             if (POST) {
-                float mean, rstd;
-                normalize<V, FULL, L>(t, p.post, inv, n, v, mean, rstd);
-                if (p.stats && live && t.leader) p.stats[2 * p.rows + row] = mean, p.stats[3 * p.rows + row] = rstd;
+                float mean;
+                normalize<V, FULL, L>(t, p.post, inv, n, v, mean, r);
+                if (p.stats && live && t.leader) p.stats[2 * p.rows + row] = mean, p.stats[3 * p.rows + row] = r;
             }
-            if (p.fc.codes) bad |= row_ckpt<V, FULL, L>(p.fc, t, n, v, at);
+            if (p.fc.codes) bad |= row_ckpt<V, FULL, L>(p.fc, t, n, v, r, at);
             if (p.has_cw) {
 #pragma unroll
                 for (int i = 0; i < V; i++) {
@@ -221,9 +218,10 @@ __global__ void __launch_bounds__(kFwdThreads, 1) k_norm_fwd(const __grid_consta
                         if (FULL || i < have) plane_get(plane_cb, p.nvec, i * L + t.first_vec, w);
                         else zero8(w);
 #pragma unroll
-                        for (int j = 0; j < 4; j++) v[i][j] = f2_add(v[i][j], w[j]);
+                        for (int j = 0; j < 4; j++) v[i][j] = f2_fma(v[i][j], f2_of(r, r), w[j]);
                     }
                 }
+                if (p.has_cb) r = 1.0f;
                 if (p.several && live) {
 #pragma unroll
                     for (int i = 0; i < V; i++) {
@@ -235,20 +233,20 @@ __global__ void __launch_bounds__(kFwdThreads, 1) k_norm_fwd(const __grid_consta
                     }
                 }
             } else {
-                const f2 s2 = f2_of(p.s, p.s);
-#pragma unroll
-                for (int i = 0; i < V; i++)
-#pragma unroll
-                    for (int j = 0; j < 4; j++) v[i][j] = f2_mul(v[i][j], s2);
+                r *= p.s;
             }
-            const f2 a2 = f2_of(p.a, p.a);
+            // x' = a x + r v
 #pragma unroll
             for (int i = 0; i < V; i++) {
                 f2 xx[4];
                 if (FULL || i < n) ring_row8<XT, N>(stage + i * kSlots<XT> * N * 16, xx);
                 else zero8(xx);
+                if (p.a != 1.0f) {
 #pragma unroll
-                for (int j = 0; j < 4; j++) v[i][j] = f2_fma(xx[j], a2, v[i][j]);
+                    for (int j = 0; j < 4; j++) xx[j] = f2_mul(xx[j], f2_of(p.a, p.a));
+                }
+#pragma unroll
+                for (int j = 0; j < 4; j++) v[i][j] = f2_fma(v[i][j], f2_of(r, r), xx[j]);
             }
             if (p.xo && live) {
 #pragma unroll
@@ -263,10 +261,10 @@ __global__ void __launch_bounds__(kFwdThreads, 1) k_norm_fwd(const __grid_consta
             }
         }
         if (PRE) {
-            float mean, rstd;
-            normalize<V, FULL, L>(t, p.pre, inv, n, v, mean, rstd);
-            if (p.stats && live && t.leader) p.stats[row] = mean, p.stats[p.rows + row] = rstd;
-            if (p.xc.codes) bad |= row_ckpt<V, FULL, L>(p.xc, t, n, v, at);
+            float mean;
+            normalize<V, FULL, L>(t, p.pre, inv, n, v, mean, r);
+            if (p.stats && live && t.leader) p.stats[row] = mean, p.stats[p.rows + row] = r;
+            if (p.xc.codes) bad |= row_ckpt<V, FULL, L>(p.xc, t, n, v, r, at);
             if (p.pre.w) {
 #pragma unroll
                 for (int i = 0; i < V; i++) {
@@ -284,8 +282,13 @@ __global__ void __launch_bounds__(kFwdThreads, 1) k_norm_fwd(const __grid_consta
                     if (FULL || i < have) plane_get(plane_pb, p.nvec, i * L + t.first_vec, w);
                     else zero8(w);
 #pragma unroll
-                    for (int j = 0; j < 4; j++) v[i][j] = f2_add(v[i][j], w[j]);
+                    for (int j = 0; j < 4; j++) v[i][j] = f2_fma(v[i][j], f2_of(r, r), w[j]);
                 }
+            } else {
+#pragma unroll
+                for (int i = 0; i < V; i++)
+#pragma unroll
+                    for (int j = 0; j < 4; j++) v[i][j] = f2_mul(v[i][j], f2_of(r, r));
             }
             uint4 q[V];
 #pragma unroll
