@@ -17,7 +17,7 @@ __device__ __forceinline__ int64_t place(int64_t i, int64_t nvec, int64_t ld)
 }
 
 template <class T, int U>
-__global__ void __launch_bounds__(kEw) k_ckpt_store(const T *src, int64_t ld, int64_t total, int64_t nvec, const CkptOut out, uint32_t *dev_status)
+__global__ void __launch_bounds__(kEw) k_ckpt_store(const T *src, int64_t ld, int64_t total, int64_t nvec, bool wide, const CkptOut out, uint32_t *dev_status)
 {
     pdl_launch_dependents();
     pdl_wait();
@@ -27,7 +27,7 @@ __global__ void __launch_bounds__(kEw) k_ckpt_store(const T *src, int64_t ld, in
     for (int u = 0; u < U; u++) {
         const int64_t i = i0 + u * kEw;
         raw[u].zero();
-        if (i < total) raw[u].load(src + place(i, nvec, ld));
+        if (i < total) raw[u].load(src + place(i, nvec, ld), wide);
     }
     bool bad = false;
 #pragma unroll
@@ -42,7 +42,7 @@ __global__ void __launch_bounds__(kEw) k_ckpt_store(const T *src, int64_t ld, in
 }
 
 template <class T, int U>
-__global__ void __launch_bounds__(kEw) k_ckpt_load(const uint8_t *codes, const uint8_t *scales, int64_t total, int64_t nvec, T *dst, int64_t ld)
+__global__ void __launch_bounds__(kEw) k_ckpt_load(const uint8_t *codes, const uint8_t *scales, int64_t total, int64_t nvec, T *dst, int64_t ld, bool wide)
 {
     pdl_launch_dependents();
     pdl_wait();
@@ -57,7 +57,7 @@ __global__ void __launch_bounds__(kEw) k_ckpt_load(const uint8_t *codes, const u
         if (i >= total) continue;
         f2 v[4];
         raw[u].get(v);
-        store8(dst + place(i, nvec, ld), v);
+        store8(dst + place(i, nvec, ld), v, wide);
     }
 }
 
@@ -250,10 +250,10 @@ mxfp4_status_t mxfp4_checkpoint_store(const void *src, int32_t dtype, int64_t ld
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (dtype == MXFP4_OUT_FP32) {
         if ((s = blocks_of(total, 2, &blocks))) return s;
-        MX_CHECK_CUDA(launch_pdl(k_ckpt_store<float, 2>, blocks, 1, kEw, 0, st, static_cast<const float *>(src), ld, total, nvec, out, dev_status));
+        MX_CHECK_CUDA(launch_pdl(k_ckpt_store<float, 2>, blocks, 1, kEw, 0, st, static_cast<const float *>(src), ld, total, nvec, rows_on_32(src, ld), out, dev_status));
     } else {
         if ((s = blocks_of(total, 4, &blocks))) return s;
-        MX_CHECK_CUDA(launch_pdl(k_ckpt_store<__nv_bfloat16, 4>, blocks, 1, kEw, 0, st, static_cast<const __nv_bfloat16 *>(src), ld, total, nvec, out, dev_status));
+        MX_CHECK_CUDA(launch_pdl(k_ckpt_store<__nv_bfloat16, 4>, blocks, 1, kEw, 0, st, static_cast<const __nv_bfloat16 *>(src), ld, total, nvec, false, out, dev_status));
     }
     return MXFP4_OK;
 }
@@ -270,8 +270,8 @@ mxfp4_status_t mxfp4_checkpoint_load(mxfp4_ckpt_t src, void *dst, int32_t dtype,
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const uint8_t *codes = src.codes, *scales = src.scales;
     if ((s = blocks_of(total, 4, &blocks))) return s;
-    if (dtype == MXFP4_OUT_FP32) MX_CHECK_CUDA(launch_pdl(k_ckpt_load<float, 4>, blocks, 1, kEw, 0, st, codes, scales, total, nvec, static_cast<float *>(dst), ld));
-    else MX_CHECK_CUDA(launch_pdl(k_ckpt_load<__nv_bfloat16, 4>, blocks, 1, kEw, 0, st, codes, scales, total, nvec, static_cast<__nv_bfloat16 *>(dst), ld));
+    if (dtype == MXFP4_OUT_FP32) MX_CHECK_CUDA(launch_pdl(k_ckpt_load<float, 4>, blocks, 1, kEw, 0, st, codes, scales, total, nvec, static_cast<float *>(dst), ld, rows_on_32(dst, ld)));
+    else MX_CHECK_CUDA(launch_pdl(k_ckpt_load<__nv_bfloat16, 4>, blocks, 1, kEw, 0, st, codes, scales, total, nvec, static_cast<__nv_bfloat16 *>(dst), ld, false));
     return MXFP4_OK;
 }
 

@@ -61,24 +61,37 @@ __device__ __forceinline__ uint4 pack8(const f2 (&v)[4]) { return make_uint4(pac
 template <class T> struct Raw8;
 template <> struct Raw8<__nv_bfloat16> {
     uint4 a;
-    __device__ __forceinline__ void load(const __nv_bfloat16 *p) { a = ld_stream_16(p); }
+    __device__ __forceinline__ void load(const __nv_bfloat16 *p, bool = false) { a = ld_stream_16(p); }
     __device__ __forceinline__ void zero() { a = make_uint4(0, 0, 0, 0); }
     __device__ __forceinline__ void get(f2 (&o)[4]) const { unpack8(a, o); }
 };
 template <> struct Raw8<float> {
-    uint4 a, b;
-    __device__ __forceinline__ void load(const float *p) { a = ld_stream_16(p), b = ld_stream_16(p + 4); }
-    __device__ __forceinline__ void zero() { a = b = make_uint4(0, 0, 0, 0); }
-    __device__ __forceinline__ void get(f2 (&o)[4]) const
+    f2 v[4];
+    __device__ __forceinline__ void load(const float *p, bool wide = false)       // (wide: see store8)
     {
-        o[0] = (f2)a.y << 32 | a.x, o[1] = (f2)a.w << 32 | a.z, o[2] = (f2)b.y << 32 | b.x, o[3] = (f2)b.w << 32 | b.z;
+        if (wide) {
+            asm volatile("ld.global.L1::no_allocate.v4.b64 {%0, %1, %2, %3}, [%4];" : "=l"(v[0]), "=l"(v[1]), "=l"(v[2]), "=l"(v[3]) : "l"(p));
+        } else {
+            const uint4 a = ld_stream_16(p), b = ld_stream_16(p + 4);
+            v[0] = (f2)a.y << 32 | a.x, v[1] = (f2)a.w << 32 | a.z, v[2] = (f2)b.y << 32 | b.x, v[3] = (f2)b.w << 32 | b.z;
+        }
     }
+    __device__ __forceinline__ void zero() { v[0] = v[1] = v[2] = v[3] = 0; }
+    __device__ __forceinline__ void get(f2 (&o)[4]) const { o[0] = v[0], o[1] = v[1], o[2] = v[2], o[3] = v[3]; }
 };
 __device__ __forceinline__ void store8(__nv_bfloat16 *p, const f2 (&v)[4]) { *reinterpret_cast<uint4 *>(p) = pack8(v); }
 __device__ __forceinline__ void store8(float *p, const f2 (&v)[4])
 {
     reinterpret_cast<ulonglong2 *>(p)[0] = make_ulonglong2(v[0], v[1]);
     reinterpret_cast<ulonglong2 *>(p)[1] = make_ulonglong2(v[2], v[3]);
+}
+// `wide`: the address is a multiple of 32 bytes.  Eight FP32 values then go in one access: as two, each would touch every 32-byte sector of
+// the warp's kilobyte and the L2 would see all of them twice (x + f of 50432 x 1024 in FP32: 112 us that way).
+__device__ __forceinline__ void store8(__nv_bfloat16 *p, const f2 (&v)[4], bool) { store8(p, v); }
+__device__ __forceinline__ void store8(float *p, const f2 (&v)[4], bool wide)
+{
+    if (wide) asm volatile("st.global.v4.b64 [%0], {%1, %2, %3, %4};" ::"l"(p), "l"(v[0]), "l"(v[1]), "l"(v[2]), "l"(v[3]) : "memory");
+    else store8(p, v);
 }
 
 // ---- the format ----
@@ -174,6 +187,8 @@ struct RawCkpt {
 };
 
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+// Whether every eighth element of every row of an FP32 matrix lies on 32 bytes.
+inline bool rows_on_32(const void *p, int64_t ld) { return ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)(ld * 4)) & 31u) == 0; }
 inline int64_t dtype_bytes(int dtype) { return dtype == MXFP4_OUT_FP32 ? 4 : 2; }
 inline Span span_of_rows(const void *p, int64_t ld, int64_t rows, int64_t cols, int64_t bytes) { return span_of(p, p && rows > 0 ? bytes * ((rows - 1) * ld + cols) : 0); }
 

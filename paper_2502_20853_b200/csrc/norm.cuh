@@ -26,6 +26,7 @@ constexpr int bwd_threads(int v, int sums) { return v == 2 ? (sums == 2 ? 512 : 
 __device__ __forceinline__ void async16(uint32_t dst, const void *src) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory"); }
 __device__ __forceinline__ void async8(uint32_t dst, const void *src) { asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory"); }
 __device__ __forceinline__ void async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void warp_sync() { asm volatile("bar.warp.sync 0xffffffff;" ::: "memory"); }
 template <int LEFT> __device__ __forceinline__ void async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
 __device__ __forceinline__ uint4 lds16(uint32_t at)
 {
@@ -39,12 +40,20 @@ __device__ __forceinline__ uint2 lds8(uint32_t at)
     asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at));
     return v;
 }
-// Eight elements of type T: slots of 16 bytes per lane, one (bf16) or two (fp32) of them.  The block's N lanes lie side by side.
+// Eight elements of type T: slots of 16 bytes per lane, one (bf16) or two (fp32) of them.  The block's N lanes lie side by side; `slot` is the
+// lane's first one.  The two halves of a lane's FP32 elements are copied by it and its neighbour, so that each of the two copies of the pair
+// covers whole 32-byte sectors (a lane that copied both of its own would have the L2 read every sector twice): they become visible by the
+// warp's barrier, and the second slots of a pair are exchanged to keep off each other's banks.
 template <class T> constexpr int kSlots = sizeof(T) / 2;
 template <class T, int N> __device__ __forceinline__ void async_row8(uint32_t slot, const T *src)
 {
-    async16(slot, src);
-    if (sizeof(T) == 4) async16(slot + N * 16, src + 4);
+    if (sizeof(T) == 2) {
+        async16(slot, src);
+    } else {
+        const int odd = threadIdx.x & 1;
+        async16(slot + (odd ? N * 16 : 0), src - 4 * odd);
+        async16(slot + (odd ? N * 16 - 16 : 16), src + 8 - 4 * odd);
+    }
 }
 template <class T, int N> __device__ __forceinline__ void ring_row8(uint32_t slot, f2 (&o)[4])
 {
@@ -52,9 +61,15 @@ template <class T, int N> __device__ __forceinline__ void ring_row8(uint32_t slo
     if (sizeof(T) == 2) {
         unpack8(a, o);
     } else {
-        const uint4 b = lds16(slot + N * 16);
+        const uint4 b = lds16(slot + N * 16 + (threadIdx.x & 1 ? -16 : 16));
         o[0] = (f2)a.y << 32 | a.x, o[1] = (f2)a.w << 32 | a.z, o[2] = (f2)b.y << 32 | b.x, o[3] = (f2)b.w << 32 | b.z;
     }
+}
+// A lane's own eight FP32 elements.
+template <int N> __device__ __forceinline__ void lds8f(uint32_t slot, f2 (&o)[4])
+{
+    const uint4 a = lds16(slot), b = lds16(slot + N * 16);
+    o[0] = (f2)a.y << 32 | a.x, o[1] = (f2)a.w << 32 | a.z, o[2] = (f2)b.y << 32 | b.x, o[3] = (f2)b.w << 32 | b.z;
 }
 constexpr int kRingBytes = 226 * 1024, kMostStages = 4;
 // Waits until at most `left` (0 to 3) of this lane's groups of copies are under way.

@@ -186,7 +186,7 @@ mxfp4_status_t mxfp4_residual_norm_bwd(const mxfp4_residual_norm_t *n, const mxf
     p.dx = b->dx, p.df = static_cast<__nv_bfloat16 *>(b->df_bf16), p.lddx = b->lddx, p.lddf = b->lddf;
     p.pre = side_of(n->pre), p.post = side_of(n->post);
     p.gate = n->gate, p.ldg = n->ld_gate, p.gate_fp32 = n->gate_dtype == MXFP4_OUT_FP32;
-    p.several = n->gates > 1, p.rows_per_gate = (uint32_t)(n->gates > 1 ? rows / n->gates : rows);
+    p.several = n->gates > 1, p.wide = rows_on_32(b->dx, b->lddx), p.rows_per_gate = (uint32_t)(n->gates > 1 ? rows / n->gates : rows);
     p.a = n->residual_scale, p.s = n->branch_scale;
     p.part = static_cast<float *>(workspace), p.slots = p.part + part_floats(plan, cols), p.heads = p.slots + ((int64_t)plan.blocks + n->gates) * 2 * cols;
     p.rows = rows, p.rows_per_team = plan.rows_per_team, p.cols = (int)cols, p.nvec = (int)(cols / 8), p.warps = plan.warps(), p.teams = plan.teams;

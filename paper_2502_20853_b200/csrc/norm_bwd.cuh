@@ -21,6 +21,7 @@ struct NormBwd {
     int64_t ldg;
     uint32_t rows_per_gate;   // rows of one gate (all rows where there are not several)
     int gate_fp32;
+    int wide;                 // dx in FP32 lies on 32 bytes
     int several;              // gates: A and B are kept apart by gate
     float a, s;
     float *part;              // [blocks][4][cols]: sums of dh x^, dh, t f^ (B), t (A)
@@ -189,6 +190,7 @@ __global__ void __launch_bounds__(bwd_threads(V, 2 + SB + SA), 1) k_norm_bwd(con
         const int64_t row = first + k;
         const bool live = EXACT || row < end;
         const int n = live ? have : 0;
+        if (sizeof(XT) == 4) warp_sync();      // the neighbour has read what is overwritten
         fetch(row + S - 1, base + (slot == 0 ? S - 1 : slot - 1) * Ring::kStage);
         const uint32_t stage = base + slot * Ring::kStage;
         slot = slot == S - 1 ? 0 : slot + 1;
@@ -206,6 +208,7 @@ __global__ void __launch_bounds__(bwd_threads(V, 2 + SB + SA), 1) k_norm_bwd(con
         for (int i = 0; i < V; i++) xsc[i] = ckpt_scale(xs[i]), fsc[i] = ckpt_scale(fs[i]);
         fetch_small(row + 1);
         async_wait<S - 1>();
+        if (sizeof(XT) == 4) warp_sync();
         f2 xh[V][4], d[V][4];
 #pragma unroll
         for (int i = 0; i < V; i++) {
@@ -235,7 +238,7 @@ __global__ void __launch_bounds__(bwd_threads(V, 2 + SB + SA), 1) k_norm_bwd(con
 #pragma unroll
             for (int i = 0; i < V; i++) {
                 f2 w[4];
-                ring_row8<float, N>(w_at + i * N * 32, w);
+                lds8f<N>(w_at + i * N * 32, w);
                 c1[i] = c2[i] = 0;
 #pragma unroll
                 for (int j = 0; j < 4; j++) {
@@ -267,12 +270,12 @@ __global__ void __launch_bounds__(bwd_threads(V, 2 + SB + SA), 1) k_norm_bwd(con
             }
             if (on) {
                 if (p.a == 1.0f) {
-                    store8(dx + i * L * 8, x);
+                    store8(dx + i * L * 8, x, p.wide);
                 } else {
                     f2 y[4];
 #pragma unroll
                     for (int j = 0; j < 4; j++) y[j] = f2_mul(x[j], f2_of(p.a, p.a));
-                    store8(dx + i * L * 8, y);
+                    store8(dx + i * L * 8, y, p.wide);
                 }
             }
             // the branch: from here on xh is f^, and d the gradient of f^, then of f
@@ -291,7 +294,7 @@ __global__ void __launch_bounds__(bwd_threads(V, 2 + SB + SA), 1) k_norm_bwd(con
                     }
                 }
                 f2 w[4];
-                ring_row8<float, N>(g_at + i * N * 32, w);
+                lds8f<N>(g_at + i * N * 32, w);
 #pragma unroll
                 for (int j = 0; j < 4; j++) {
                     B[i][j] = f2_fma(x[j], xh[i][j], B[i][j]);

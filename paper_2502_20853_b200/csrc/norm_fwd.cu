@@ -49,7 +49,7 @@ mxfp4_status_t mxfp4_residual_norm_fwd(const mxfp4_residual_norm_t *n, const voi
     p.x = x, p.f = static_cast<const __nv_bfloat16 *>(f_bf16), p.xo = x_out, p.h = static_cast<__nv_bfloat16 *>(h_bf16);
     p.ldx = ldx, p.ldf = ldf, p.ldxo = ldxo, p.ldh = ldh;
     p.pre = side_of(n->pre), p.post = side_of(n->post);
-    p.gate = n->gate, p.ldg = n->ld_gate, p.gate_fp32 = n->gate_dtype == MXFP4_OUT_FP32, p.several = n->gates > 1;
+    p.gate = n->gate, p.ldg = n->ld_gate, p.gate_fp32 = n->gate_dtype == MXFP4_OUT_FP32, p.several = n->gates > 1, p.wide = rows_on_32(x_out, ldxo);
     p.has_cw = n->gate || (post && n->post.weight) || (post && n->post.bias), p.has_cb = post && n->post.bias;
     p.rows_per_gate = (uint32_t)(n->gates > 1 ? rows / n->gates : rows);
     p.a = n->residual_scale, p.s = n->branch_scale, p.stats = stats;

@@ -17,6 +17,7 @@ struct NormFwd {
     int gate_fp32, several;     // several gates
     int has_cw, has_cb;         // f^ has a factor other than s, a summand
     int stages;                 // of the ring
+    int wide;                   // x' in FP32 lies on 32 bytes
     float a, s;
     float *stats;
     CkptOut xc, fc;
@@ -179,6 +180,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) k_norm_fwd(const __grid_consta
     for (int k = 0; k < turns; k++) {
         const int64_t row = first + k;
         const bool live = EXACT || row < end;
+        if (sizeof(XT) == 4) warp_sync();      // the neighbour has read what is overwritten
         fetch(row + S - 1, ring + (slot == 0 ? S - 1 : slot - 1) * Ring::kStage);
         const uint32_t stage = ring + slot * Ring::kStage;
         slot = slot == S - 1 ? 0 : slot + 1;
@@ -188,6 +190,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) k_norm_fwd(const __grid_consta
         }
         const int n = live ? have : 0;
         async_wait_all_but(S - 1);
+        if (sizeof(XT) == 4) warp_sync();
         f2 v[V][4];
         float r = 1.0f;
         if (HAS_F) {
@@ -251,7 +254,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) k_norm_fwd(const __grid_consta
             if (p.xo && live) {
 #pragma unroll
                 for (int i = 0; i < V; i++)
-                    if (FULL || i < n) store8(xo + i * L * 8, v[i]);
+                    if (FULL || i < n) store8(xo + i * L * 8, v[i], p.wide);
             }
         } else {
 #pragma unroll
