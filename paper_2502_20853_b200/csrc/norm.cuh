@@ -40,28 +40,28 @@ __device__ __forceinline__ uint2 lds8(uint32_t at)
     asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at));
     return v;
 }
-// Eight elements of type T: slots of 16 bytes per lane, one (bf16) or two (fp32) of them.  The block's N lanes lie side by side; `slot` is the
-// lane's first one.  The two halves of a lane's FP32 elements are copied by it and its neighbour, so that each of the two copies of the pair
-// covers whole 32-byte sectors (a lane that copied both of its own would have the L2 read every sector twice): they become visible by the
-// warp's barrier, and the second slots of a pair are exchanged to keep off each other's banks.
+// Eight elements of type T: slots of 16 bytes per lane, one (bf16) or two (fp32) of them.  The block's lanes lie side by side in `slots`.  FP32 elements are copied in the order of memory, half of the L lanes' share at a time, which are not each lane's own
+// (a lane that copied both of its own would have the L2 read every sector twice, and so would any other order in shared memory): they
+// become visible by the warp's barrier.  `lanes`: the first so many have something to copy.
 template <class T> constexpr int kSlots = sizeof(T) / 2;
-template <class T, int N> __device__ __forceinline__ void async_row8(uint32_t slot, const T *src)
+template <class T, int L> __device__ __forceinline__ void async_row8(uint32_t slots, const T *src, int lanes)
 {
+    const int tid = threadIdx.x, l = tid & (L - 1);
     if (sizeof(T) == 2) {
-        async16(slot, src);
+        if (l < lanes) async16(slots + tid * 16, src);
     } else {
-        const int odd = threadIdx.x & 1;
-        async16(slot + (odd ? N * 16 : 0), src - 4 * odd);
-        async16(slot + (odd ? N * 16 - 16 : 16), src + 8 - 4 * odd);
+        const uint32_t to = slots + tid * 32 - l * 16;
+        if (l >> 1 < lanes) async16(to, src - 4 * l);
+        if ((l >> 1) + L / 2 < lanes) async16(to + L * 16, src - 4 * l + 4 * L);
     }
 }
-template <class T, int N> __device__ __forceinline__ void ring_row8(uint32_t slot, f2 (&o)[4])
+template <class T> __device__ __forceinline__ void ring_row8(uint32_t slots, f2 (&o)[4])
 {
-    const uint4 a = lds16(slot);
+    const uint4 a = lds16(slots + threadIdx.x * (sizeof(T) == 2 ? 16 : 32));
     if (sizeof(T) == 2) {
         unpack8(a, o);
     } else {
-        const uint4 b = lds16(slot + N * 16 + (threadIdx.x & 1 ? -16 : 16));
+        const uint4 b = lds16(slots + threadIdx.x * 32 + 16);
         o[0] = (f2)a.y << 32 | a.x, o[1] = (f2)a.w << 32 | a.z, o[2] = (f2)b.y << 32 | b.x, o[3] = (f2)b.w << 32 | b.z;
     }
 }
@@ -116,7 +116,11 @@ template <int L> struct Team {
 
 // Rows of which a team of several in a warp has none left take part in its shuffles; `turns` is the same for all teams of a warp.
 // (A warp that is in no team has no rows.)
-template <int L> __device__ __forceinline__ int turns_of(int rows_per_team, int64_t first, int64_t end) { return L < 32 ? rows_per_team : (int)(end - first); }
+template <int L> __device__ __forceinline__ int turns_of(int64_t end, int64_t first, int64_t step)
+{
+    const int64_t at = L < 32 ? first - first % step : first;     // (of the first team of several)
+    return at < end ? (int)((end - at + step - 1) / step) : 0;
+}
 
 // The sums of N (1, 2) numbers over the lanes of the team, the same bits in each of them.  All lanes of the warp take part.
 template <int N, int L>

@@ -68,6 +68,7 @@ __global__ void __launch_bounds__(bwd_threads(V, 2 + SB + SA), 1) k_norm_bwd(con
     const int64_t first = t.id < p.teams ? min(team * p.rows_per_team, p.rows) : p.rows, end = min(first + p.rows_per_team, p.rows);
     constexpr bool EXACT = FULL && L == 32;      // each turn of each lane has a row and all of its vectors
     const int have = FULL ? V : max(0, min(V, (p.nvec - t.first_vec + L - 1) / L));
+    const int lanes = p.nvec - t.first_vec + t.lane;     // vectors of the row from this part's first lane on
     const float inv = 1.0f / (float)p.cols;
     const uint32_t base = (uint32_t)__cvta_generic_to_shared(s_ring);
     const uint32_t at16 = threadIdx.x * 16, at8 = threadIdx.x * 8;
@@ -80,19 +81,19 @@ __global__ void __launch_bounds__(bwd_threads(V, 2 + SB + SA), 1) k_norm_bwd(con
     const auto fetch = [&](int64_t row, uint32_t stage) {
         if (row < end) {
 #pragma unroll
-            for (int i = 0; i < V; i++)
-                if (FULL || i < have) {
-                    if (p.dxo) async_row8<XT, N>(stage + at16 + i * kSlots<XT> * N * 16, dxo_at + i * L * 8);
-                    if (PRE) {
-                        async_row8<__nv_bfloat16, N>(stage + Ring::kDh + at16 + i * N * 16, dh_at + i * L * 8);
-                        if (EIGHT) async8(stage + Ring::kXh + at8 + i * N * 8, xc_at + i * L * 8);
-                        else async_row8<XT, N>(stage + Ring::kXh + at16 + i * kSlots<XT> * N * 16, xo_at + i * L * 8);
-                    }
-                    if (NEED_F) {
-                        if (EIGHT) async8(stage + Ring::kFh + at8 + i * N * 8, fc_at + i * L * 8);
-                        else async_row8<__nv_bfloat16, N>(stage + Ring::kFh + at16 + i * N * 16, f_at + i * L * 8);
-                    }
+            for (int i = 0; i < V; i++) {
+                const int l = FULL ? L : lanes - i * L;
+                if (p.dxo) async_row8<XT, L>(stage + i * kSlots<XT> * N * 16, dxo_at + i * L * 8, l);
+                if (PRE) {
+                    async_row8<__nv_bfloat16, L>(stage + Ring::kDh + i * N * 16, dh_at + i * L * 8, l);
+                    if (!EIGHT) async_row8<XT, L>(stage + Ring::kXh + i * kSlots<XT> * N * 16, xo_at + i * L * 8, l);
+                    else if (FULL || i < have) async8(stage + Ring::kXh + at8 + i * N * 8, xc_at + i * L * 8);
                 }
+                if (NEED_F) {
+                    if (!EIGHT) async_row8<__nv_bfloat16, L>(stage + Ring::kFh + i * N * 16, f_at + i * L * 8, l);
+                    else if (FULL || i < have) async8(stage + Ring::kFh + at8 + i * N * 8, fc_at + i * L * 8);
+                }
+            }
             dxo_at += p.lddxo;
             if (PRE) dh_at += p.lddh;
             if (PRE && EIGHT) xc_at += p.cols;
@@ -185,12 +186,12 @@ __global__ void __launch_bounds__(bwd_threads(V, 2 + SB + SA), 1) k_norm_bwd(con
     uint32_t slot = 0;
     XT *dx = static_cast<XT *>(p.dx) + first * p.lddx + t.first_vec * 8;       // the lane's places in this row
     __nv_bfloat16 *df = p.df + first * p.lddf + t.first_vec * 8;
-    const int turns = turns_of<L>((int)p.rows_per_team, first, end);
+    const int turns = L < 32 ? (int)p.rows_per_team : (int)(end - first);
     for (int k = 0; k < turns; k++, dx += p.lddx, df += p.lddf) {
         const int64_t row = first + k;
         const bool live = EXACT || row < end;
         const int n = live ? have : 0;
-        if (sizeof(XT) == 4) warp_sync();      // the neighbour has read what is overwritten
+        if (sizeof(XT) == 4) warp_sync();      // the others have read what is overwritten
         fetch(row + S - 1, base + (slot == 0 ? S - 1 : slot - 1) * Ring::kStage);
         const uint32_t stage = base + slot * Ring::kStage;
         slot = slot == S - 1 ? 0 : slot + 1;
@@ -214,11 +215,11 @@ __global__ void __launch_bounds__(bwd_threads(V, 2 + SB + SA), 1) k_norm_bwd(con
         for (int i = 0; i < V; i++) {
             if (PRE) {
                 if (FULL || i < n) {
-                    ring_row8<__nv_bfloat16, N>(stage + Ring::kDh + at16 + i * N * 16, d[i]);
+                    ring_row8<__nv_bfloat16>(stage + Ring::kDh + i * N * 16, d[i]);
                     if (EIGHT) {
                         e4m3_to8(lds8(stage + Ring::kXh + at8 + i * N * 8), xsc[i], xh[i]);
                     } else {
-                        ring_row8<XT, N>(stage + Ring::kXh + at16 + i * kSlots<XT> * N * 16, xh[i]);
+                        ring_row8<XT>(stage + Ring::kXh + i * kSlots<XT> * N * 16, xh[i]);
                         const f2 m2 = f2_of(-pm0, -pm0), r2 = f2_of(pr0, pr0);
 #pragma unroll
                         for (int j = 0; j < 4; j++) xh[i][j] = f2_mul(f2_add(xh[i][j], m2), r2);
@@ -262,7 +263,7 @@ __global__ void __launch_bounds__(bwd_threads(V, 2 + SB + SA), 1) k_norm_bwd(con
         for (int i = 0; i < V; i++) {
             const bool on = FULL ? live : i < n;
             f2 x[4];
-            if (on) ring_row8<XT, N>(stage + at16 + i * kSlots<XT> * N * 16, x);
+            if (on) ring_row8<XT>(stage + i * kSlots<XT> * N * 16, x);
             else zero8(x);
             if (PRE && on) {
 #pragma unroll
@@ -286,7 +287,7 @@ __global__ void __launch_bounds__(bwd_threads(V, 2 + SB + SA), 1) k_norm_bwd(con
                 } else if (EIGHT) {
                     e4m3_to8(lds8(stage + Ring::kFh + at8 + i * N * 8), fsc[i], xh[i]);
                 } else {
-                    ring_row8<__nv_bfloat16, N>(stage + Ring::kFh + at16 + i * N * 16, xh[i]);
+                    ring_row8<__nv_bfloat16>(stage + Ring::kFh + i * N * 16, xh[i]);
                     if (POST) {
                         const f2 n2 = f2_of(-qm0, -qm0), r2 = f2_of(qr0, qr0);
 #pragma unroll

@@ -116,12 +116,16 @@ __global__ void __launch_bounds__(kFwdThreads, 1) k_norm_fwd(const __grid_consta
     pdl_launch_dependents();
     Team<L> t(p.warps, V, s_sum);
     const int64_t team = (int64_t)blockIdx.x * p.teams + t.id;
-    const int64_t first = t.id < p.teams ? min(team * p.rows_per_team, p.rows) : p.rows, end = min(first + p.rows_per_team, p.rows);
+    // rows first, first + step, ...: all teams side by side (what they read at a time lies together: 401408 x 96 in runs of rows 98 us, so
+    // 74), with several gates the block's teams in a run of rows, which share the gate
+    const int64_t run = (int64_t)blockIdx.x * p.teams * p.rows_per_team, end = p.several ? min(run + p.teams * p.rows_per_team, p.rows) : p.rows;
+    const int64_t step = p.several ? p.teams : (int64_t)gridDim.x * p.teams, first = t.id < p.teams ? (p.several ? run + t.id : team) : p.rows;
     constexpr bool EXACT = FULL && L == 32;      // each turn of each lane has a row and all of its vectors
     const int have = FULL ? V : max(0, min(V, (p.nvec - t.first_vec + L - 1) / L));   // vectors of this lane
+    const int lanes = p.nvec - t.first_vec + t.lane;     // vectors of the row from this part's first lane on
     const float inv = 1.0f / (float)p.cols;
     const int S = p.stages;
-    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(s_ring) + threadIdx.x * 16;
+    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(s_ring);
     float4 *const plane_cw = reinterpret_cast<float4 *>(s_ring + S * Ring::kStage), *const plane_cb = plane_cw + (p.has_cw ? 2 * p.nvec : 0);
     float4 *const plane_pw = plane_cb + (p.has_cb ? 2 * p.nvec : 0), *const plane_pb = plane_pw + (p.pre.w ? 2 * p.nvec : 0);
     pdl_wait();
@@ -132,18 +136,18 @@ __global__ void __launch_bounds__(kFwdThreads, 1) k_norm_fwd(const __grid_consta
         if (row < end) {
 #pragma unroll
             for (int i = 0; i < V; i++)
-                if (FULL || i < have) async_row8<XT, N>(stage + i * kSlots<XT> * N * 16, xp + i * L * 8);
+                async_row8<XT, L>(stage + i * kSlots<XT> * N * 16, xp + i * L * 8, FULL ? L : lanes - i * L);
             if (HAS_F) {
 #pragma unroll
                 for (int i = 0; i < V; i++)
-                    if (FULL || i < have) async_row8<__nv_bfloat16, N>(stage + Ring::kF + i * N * 16, fp + i * L * 8);
-                fp += p.ldf;
+                    async_row8<__nv_bfloat16, L>(stage + Ring::kF + i * N * 16, fp + i * L * 8, FULL ? L : lanes - i * L);
+                fp += step * p.ldf;
             }
-            xp += p.ldx;
+            xp += step * p.ldx;
         }
         async_commit();
     };
-    for (int k = 0; k < S - 1; k++) fetch(first + k, ring + k * Ring::kStage);
+    for (int k = 0; k < S - 1; k++) fetch(first + k * step, ring + k * Ring::kStage);
 
     for (int vec = threadIdx.x; vec < p.nvec; vec += N) {
         f2 w[4], b[4];
@@ -169,25 +173,19 @@ __global__ void __launch_bounds__(kFwdThreads, 1) k_norm_fwd(const __grid_consta
     }
     __syncthreads();
 
-    uint32_t gate = p.several ? (uint32_t)first / p.rows_per_gate : 0u;
-    uint32_t left = p.several ? p.rows_per_gate - ((uint32_t)first - gate * p.rows_per_gate) : 0u;   // rows of this gate still to come
     bool bad = false;
     int slot = 0;
     int64_t at = first * p.nvec + t.first_vec;      // this row's place in a checkpoint
     XT *xo = static_cast<XT *>(p.xo) + first * p.ldxo + t.first_vec * 8;
     __nv_bfloat16 *h = p.h + first * p.ldh + t.first_vec * 8;
-    const int turns = turns_of<L>((int)p.rows_per_team, first, end);
+    const int turns = turns_of<L>(end, first, step);
     for (int k = 0; k < turns; k++) {
-        const int64_t row = first + k;
+        const int64_t row = first + k * step;
         const bool live = EXACT || row < end;
-        if (sizeof(XT) == 4) warp_sync();      // the neighbour has read what is overwritten
-        fetch(row + S - 1, ring + (slot == 0 ? S - 1 : slot - 1) * Ring::kStage);
+        if (sizeof(XT) == 4) warp_sync();      // the others have read what is overwritten
+        fetch(row + (S - 1) * step, ring + (slot == 0 ? S - 1 : slot - 1) * Ring::kStage);
         const uint32_t stage = ring + slot * Ring::kStage;
         slot = slot == S - 1 ? 0 : slot + 1;
-        if (HAS_F && p.several && live) {
-            if (left == 0) gate++, left = p.rows_per_gate;
-            left--;
-        }
         const int n = live ? have : 0;
         async_wait_all_but(S - 1);
         if (sizeof(XT) == 4) warp_sync();
@@ -196,7 +194,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) k_norm_fwd(const __grid_consta
         if (HAS_F) {
 #pragma unroll
             for (int i = 0; i < V; i++) {
-                if (FULL || i < n) ring_row8<__nv_bfloat16, N>(stage + Ring::kF + i * N * 16, v[i]);
+                if (FULL || i < n) ring_row8<__nv_bfloat16>(stage + Ring::kF + i * N * 16, v[i]);
                 else zero8(v[i]);
             }
             if (POST) {
@@ -226,6 +224,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) k_norm_fwd(const __grid_consta
                 }
                 if (p.has_cb) r = 1.0f;
                 if (p.several && live) {
+                    const int64_t gate = (uint32_t)row / p.rows_per_gate;
 #pragma unroll
                     for (int i = 0; i < V; i++) {
                         f2 g[4];
@@ -242,7 +241,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) k_norm_fwd(const __grid_consta
 #pragma unroll
             for (int i = 0; i < V; i++) {
                 f2 xx[4];
-                if (FULL || i < n) ring_row8<XT, N>(stage + i * kSlots<XT> * N * 16, xx);
+                if (FULL || i < n) ring_row8<XT>(stage + i * kSlots<XT> * N * 16, xx);
                 else zero8(xx);
                 if (p.a != 1.0f) {
 #pragma unroll
@@ -259,7 +258,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) k_norm_fwd(const __grid_consta
         } else {
 #pragma unroll
             for (int i = 0; i < V; i++) {
-                if (FULL || i < n) ring_row8<XT, N>(stage + i * kSlots<XT> * N * 16, v[i]);
+                if (FULL || i < n) ring_row8<XT>(stage + i * kSlots<XT> * N * 16, v[i]);
                 else zero8(v[i]);
             }
         }
@@ -325,7 +324,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) k_norm_fwd(const __grid_consta
                         for (int b = t.lane; b < p.nblk4 * 4; b += L) p.hq_scales[scale_offset(r, b, p.nblk4)] = 0x7F;
             }
         }
-        at += p.nvec, xo += p.ldxo, h += p.ldh;
+        at += step * p.nvec, xo += step * p.ldxo, h += step * p.ldh;
     }
     if (bad && p.dev_status) atomicOr(p.dev_status, MXFP4_DEV_NONFINITE);
 }
