@@ -4,12 +4,16 @@
 // through shuffles and, where a team has several warps, through shared memory and a barrier of the team.  V (2 to 4
 // backward, 3 or 4 forward) and the lanes are chosen so that a block's lanes have the most to do (row_plan); the usual widths are reached
 // exactly.
-// One block per SM; each team takes a run of consecutive rows, so that its lanes keep their columns: what belongs to a column (weights,
-// a gate, sums over rows) is fetched once.  The few warps cannot hide the memory's latency by themselves; a lane's share of the next
-// rows travels into shared memory meanwhile (cp.async into slots that only this lane reads: no barriers).
+// Two blocks per SM, and for long matrices several times as many blocks as fit: the SMs do not get equal shares of the memory's bandwidth (in
+// a kernel of one block per SM the mean SM was done at 81 % of the last one's time), so what is left is dealt out as they finish.  A block's
+// lanes keep their columns from row to row: what belongs to a column (weights, a gate, sums over rows) is fetched once.  The few warps
+// cannot hide the memory's latency by themselves; a lane's share of the next rows travels into shared memory meanwhile (cp.async, mostly
+// into slots that only this lane reads: no barriers of the block).
 // FULL: T V vectors are exactly a row.  The kernels are bound by the instructions they issue, and without the masks of a partly filled
 // lane the loops over V are straight code.
 #pragma once
+#include <algorithm>
+
 #include "ckpt.cuh"
 #include "quant_tile.cuh"
 #include "tma.cuh"
@@ -17,10 +21,11 @@
 namespace mx {
 
 constexpr int kNormMaxCols = 8192;
-constexpr int kFwdThreads = 512;
+constexpr int kFwdThreads = 256;
 // Backward: as many warps as the registers allow for v vectors of a lane and `sums` sums over rows (8 v registers each).  A kernel that
 // spills is twice as slow (50432 x 768: 80 us with eight warps, 158 with twelve and 200 bytes of spills): the ring leaves no L1 for them.
-constexpr int bwd_threads(int v, int sums) { return v == 2 ? (sums == 2 ? 512 : 384) : v == 3 && sums == 2 ? 384 : 256; }
+constexpr int bwd_threads(int v, int sums) { return v == 4 ? 256 : v == 2 ? (sums == 2 ? 256 : 192) : sums == 2 ? 192 : 128; }
+constexpr int bwd_blocks_per_sm(int v) { return v == 4 ? 1 : 2; }
 
 // ---- a lane's ring of rows in shared memory ----------------------------------------------------
 __device__ __forceinline__ void async16(uint32_t dst, const void *src) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory"); }
@@ -71,7 +76,7 @@ template <int N> __device__ __forceinline__ void lds8f(uint32_t slot, f2 (&o)[4]
     const uint4 a = lds16(slot), b = lds16(slot + N * 16);
     o[0] = (f2)a.y << 32 | a.x, o[1] = (f2)a.w << 32 | a.z, o[2] = (f2)b.y << 32 | b.x, o[3] = (f2)b.w << 32 | b.z;
 }
-constexpr int kRingBytes = 226 * 1024, kMostStages = 4;
+constexpr int kRingBytes = 226 * 1024, kHalfRingBytes = 112 * 1024, kMostStages = 4;     // of an SM's one block, of one of two
 // Waits until at most `left` (0 to 3) of this lane's groups of copies are under way.
 __device__ __forceinline__ void async_wait_all_but(int left)
 {
@@ -173,8 +178,9 @@ __device__ __forceinline__ void load_side8(const NormSide &n, int vec, f2 (&w)[4
 }
 
 // ---- host -----------------------------------------------------------------------------------------
-// Blocks (one per SM of a B200) and the consecutive rows of one team.  By the shape alone: the backward pass's workspace is laid out by it.
-constexpr int kBlocks = 148;
+constexpr int kSms = 148;      // of a B200; the plan goes by the shape alone, for the backward pass's workspace is laid out by it
+
+// A matrix's rows on teams.
 struct RowPlan {
     int lanes, v, teams, blocks;    // lanes of a team, vectors of a lane, teams of a block
     bool full;
@@ -198,8 +204,12 @@ inline RowPlan row_plan(int64_t rows, int64_t cols, int sums)
         if (teams > 0 && (sums ? used > best : used >= best)) b.v = k, b.lanes = lanes, b.teams = teams, best = used;
     }
     b.full = (int64_t)b.v * b.lanes * 8 == cols;
-    const int64_t teams = b.teams, most = ceil_div(rows, teams);
-    b.rows_per_team = ceil_div(rows, (most < kBlocks ? most : kBlocks) * teams);
+    // forward up to three times as many blocks as are resident, as long as a team keeps six rows: 50432 x 768 with one, two, three, five times
+    // 74, 68, 69, 75 us, 8192 x 4096 48, 45, 44, 48, 25216 x 384 (five rows with one) 20.3, 24.8, 25.2, 25.2.  Backward each block has sums to
+    // leave, and more of them do not pay: 50432 x 768 with one, two, three times 75, 84, 92
+    const int64_t teams = b.teams, resident = (int64_t)kSms * (sums ? bwd_blocks_per_sm(b.v) : 2), most = ceil_div(rows, teams);
+    const int64_t times = sums ? 1 : std::min<int64_t>(std::max<int64_t>(rows / (resident * teams * 6), 1), 3);
+    b.rows_per_team = ceil_div(rows, std::min(most, resident * times) * teams);
     b.blocks = (int)ceil_div(ceil_div(rows, b.rows_per_team), teams);     // blocks that have rows
     return b;
 }
@@ -246,12 +256,6 @@ template <class F> inline cudaError_t with_bools(bool a, bool b, bool c, F &&f)
     using N = std::false_type;
     if (a) return b ? (c ? f(T(), T(), T()) : f(T(), T(), N())) : (c ? f(T(), N(), T()) : f(T(), N(), N()));
     return b ? (c ? f(N(), T(), T()) : f(N(), T(), N())) : (c ? f(N(), N(), T()) : f(N(), N(), N()));
-}
-// Stages of a ring: as many as there is room for beside `other` bytes.
-inline int ring_stages(size_t other, size_t stage)
-{
-    const size_t fit = (kRingBytes - other) / stage;
-    return (int)(fit < kMostStages ? fit : kMostStages);
 }
 // Launches a kernel of THREADS per block that may take up to kRingBytes of shared memory.
 template <auto KERNEL, int THREADS, class P> inline cudaError_t launch_ring(int blocks, size_t smem, cudaStream_t st, const P &p)

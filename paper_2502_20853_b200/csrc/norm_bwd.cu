@@ -44,19 +44,19 @@ __device__ __forceinline__ float4 gate_gradient(const NormBwdFinish &p, int c, c
     return mul4(o, all4(p.s));
 }
 
-// Adds up what the blocks and teams have left, in a fixed order.  Two kinds of blocks: the first cols / 16 take 16 columns each, 4 lanes of
-// 4 columns by 64 lanes of rows, for the sums over all rows; then, where there are several gates, one for each gate and 128 columns.
+// Adds up what the blocks and teams have left, in a fixed order.  Two kinds of blocks: the first cols / 8 take 8 columns each, 2 lanes of
+// 4 columns by 128 lanes of rows, for the sums over all rows; then, where there are several gates, one for each gate and 128 columns.
 __global__ void __launch_bounds__(256) k_norm_bwd_finish(const __grid_constant__ NormBwdFinish p)
 {
-    __shared__ float4 s_v[8][4][4], s_g[8][2][32];
+    __shared__ float4 s_v[8][4][2], s_g[8][2][32];
     pdl_launch_dependents();
     pdl_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    if ((int)blockIdx.x < p.cols / 16) {
-        const int q = threadIdx.x & 3, r = threadIdx.x >> 2, c = blockIdx.x * 16 + q * 4;
+    if ((int)blockIdx.x < p.cols / 8) {
+        const int q = threadIdx.x & 1, r = threadIdx.x >> 1, c = blockIdx.x * 8 + q * 4;
         float4 v[4] = {all4(0), all4(0), all4(0), all4(0)};     // of dh x^, dh, t f^ (with several gates times g), t (the same)
         const bool f = p.use_f && !p.several;
-        for (int k = r; k < p.blocks; k += 64) {
+        for (int k = r; k < p.blocks; k += 128) {
             const float *at = p.part + (int64_t)k * 4 * p.cols + c;
             if (p.pre) add4(v[0], load4(at));
             if (p.sb) add4(v[1], load4(at + p.cols));
@@ -64,7 +64,7 @@ __global__ void __launch_bounds__(256) k_norm_bwd_finish(const __grid_constant__
             if (f && p.sa) add4(v[3], load4(at + 3 * p.cols));
         }
         if (p.use_f && p.several && (p.dw_post || p.db_post))
-            for (int k = r; k < p.blocks; k += 64) {
+            for (int k = r; k < p.blocks; k += 128) {
                 const int64_t first = k * p.rows_per_block, end = first + p.rows_per_block < p.rows ? first + p.rows_per_block : p.rows;
                 for (uint32_t g = (uint32_t)first / (uint32_t)p.rows_per_gate; g <= (uint32_t)(end - 1) / (uint32_t)p.rows_per_gate; g++) {
                     const float *at = p.slots + (int64_t)(k + g) * 2 * p.cols + c;
@@ -75,13 +75,13 @@ __global__ void __launch_bounds__(256) k_norm_bwd_finish(const __grid_constant__
 #pragma unroll
         for (int i = 0; i < 4; i++) {
 #pragma unroll
-            for (int o = 4; o < 32; o <<= 1)
+            for (int o = 2; o < 32; o <<= 1)
                 add4(v[i], make_float4(__shfl_xor_sync(0xFFFFFFFFu, v[i].x, o), __shfl_xor_sync(0xFFFFFFFFu, v[i].y, o), __shfl_xor_sync(0xFFFFFFFFu, v[i].z, o),
                                        __shfl_xor_sync(0xFFFFFFFFu, v[i].w, o)));
-            if (lane < 4) s_v[warp][i][lane] = v[i];
+            if (lane < 2) s_v[warp][i][lane] = v[i];
         }
         __syncthreads();
-        if (threadIdx.x >= 4) return;
+        if (threadIdx.x >= 2) return;
 #pragma unroll
         for (int i = 0; i < 4; i++) {
             v[i] = s_v[0][i][q];
@@ -95,7 +95,7 @@ __global__ void __launch_bounds__(256) k_norm_bwd_finish(const __grid_constant__
         put(p.dw_post, mul4(v[2], g)), put(p.db_post, mul4(v[3], g));
         return;
     }
-    const int job = blockIdx.x - p.cols / 16;
+    const int job = blockIdx.x - p.cols / 8;
     const int64_t g = job / p.slices;
     const int c = (job - (int)g * p.slices) * 128 + lane * 4;
     const int64_t t0 = g * p.rows_per_gate / p.rows_per_block, t1 = ((g + 1) * p.rows_per_gate - 1) / p.rows_per_block;     // blocks
@@ -200,7 +200,7 @@ mxfp4_status_t mxfp4_residual_norm_bwd(const mxfp4_residual_norm_t *n, const mxf
     e.rows = rows, e.rows_per_gate = p.rows_per_gate, e.rows_per_block = plan.rows_per_team * plan.teams, e.cols = (int)cols;
     e.slices = (int)ceil_div(cols, 128);
     e.dw_pre = b->dw_pre, e.db_pre = b->db_pre, e.dw_post = b->dw_post, e.db_post = b->db_post, e.dgate = b->dgate;
-    const int64_t blocks = cols / 16 + (e.several && b->dgate ? e.gates * e.slices : 0);
+    const int64_t blocks = cols / 8 + (e.several && b->dgate ? e.gates * e.slices : 0);
     MX_CHECK_CUDA(launch_pdl(k_norm_bwd_finish, (unsigned)blocks, 1, 256, 0, st, e));
     return MXFP4_OK;
 }

@@ -40,7 +40,8 @@ template <class XT, int V, int SUMS, bool EIGHT, bool NEED_F, bool PRE> struct B
     static constexpr int kStage = kFh + (NEED_F ? (EIGHT ? 8 : 16) * kRow : 0);
     // behind the ring, also a lane's own: N_pre's weights, and s g w1 of the present gate, in FP32
     static constexpr int kW = PRE ? 32 * kRow : 0, kG = NEED_F ? 32 * kRow : 0;
-    static constexpr int kDepth = (kRingBytes - kW - kG) / kStage < kMostStages ? (kRingBytes - kW - kG) / kStage : kMostStages;
+    static constexpr int kRoom = (bwd_blocks_per_sm(V) == 2 ? kHalfRingBytes : kRingBytes) - kW - kG;
+    static constexpr int kDepth = kRoom / kStage < kMostStages ? kRoom / kStage : kMostStages;
     static constexpr int kSums = 6 * 4 * 8 * kRow;       // at the end: up to six sums per column for each warp (team)
     static constexpr int kBytes = kDepth * kStage + kW + kG > kSums ? kDepth * kStage + kW + kG : kSums;
 };
@@ -56,7 +57,7 @@ template <int N> __device__ __forceinline__ void sts8(uint32_t slot, const f2 (&
 // They go to memory once per block, A and B of several gates once per block and gate; k_norm_bwd_finish adds them up. 
 // SB, SA: the sums of dh and of t are wanted.
 template <class XT, int L, int V, bool FULL, bool EIGHT, bool NEED_F, bool POST, bool PRE, bool SB, bool SA>
-__global__ void __launch_bounds__(bwd_threads(V, 2 + SB + SA), 1) k_norm_bwd(const __grid_constant__ NormBwd p)
+__global__ void __launch_bounds__(bwd_threads(V, 2 + SB + SA), bwd_blocks_per_sm(V)) k_norm_bwd(const __grid_constant__ NormBwd p)
 {
     using Ring = BwdRing<XT, V, 2 + SB + SA, EIGHT, NEED_F, PRE>;
     constexpr int N = Ring::N, S = Ring::kDepth;
@@ -65,7 +66,9 @@ __global__ void __launch_bounds__(bwd_threads(V, 2 + SB + SA), 1) k_norm_bwd(con
     pdl_launch_dependents();
     Team<L> t(p.warps, V, s_sum);
     const int64_t team = (int64_t)blockIdx.x * p.teams + t.id;
-    const int64_t first = t.id < p.teams ? min(team * p.rows_per_team, p.rows) : p.rows, end = min(first + p.rows_per_team, p.rows);
+    // rows first, first + step, ...: side by side (see the forward pass), with several gates a run of rows for each team
+    const int64_t first = t.id < p.teams ? min(p.several ? team * p.rows_per_team : team, p.rows) : p.rows, end = p.several ? min(first + p.rows_per_team, p.rows) : p.rows;
+    const int64_t step = p.several ? 1 : (int64_t)gridDim.x * p.teams;
     constexpr bool EXACT = FULL && L == 32;      // each turn of each lane has a row and all of its vectors
     const int have = FULL ? V : max(0, min(V, (p.nvec - t.first_vec + L - 1) / L));
     const int lanes = p.nvec - t.first_vec + t.lane;     // vectors of the row from this part's first lane on
@@ -94,12 +97,12 @@ __global__ void __launch_bounds__(bwd_threads(V, 2 + SB + SA), 1) k_norm_bwd(con
                     else if (FULL || i < have) async8(stage + Ring::kFh + at8 + i * N * 8, fc_at + i * L * 8);
                 }
             }
-            dxo_at += p.lddxo;
-            if (PRE) dh_at += p.lddh;
-            if (PRE && EIGHT) xc_at += p.cols;
-            if (PRE && !EIGHT) xo_at += p.ldxo;
-            if (NEED_F && EIGHT) fc_at += p.cols;
-            if (NEED_F && !EIGHT) f_at += p.ldf;
+            dxo_at += step * p.lddxo;
+            if (PRE) dh_at += step * p.lddh;
+            if (PRE && EIGHT) xc_at += step * p.cols;
+            if (PRE && !EIGHT) xo_at += step * p.ldxo;
+            if (NEED_F && EIGHT) fc_at += step * p.cols;
+            if (NEED_F && !EIGHT) f_at += step * p.ldf;
         }
         async_commit();
     };
@@ -120,7 +123,7 @@ __global__ void __launch_bounds__(bwd_threads(V, 2 + SB + SA), 1) k_norm_bwd(con
                     if (PRE) xs[i] = xs_at[i * (L / 4)];
                     if (NEED_F) fs[i] = fs_at[i * (L / 4)];
                 }
-            xs_at += p.cols >> 5, fs_at += p.cols >> 5;
+            xs_at += step * (p.cols >> 5), fs_at += step * (p.cols >> 5);
         }
     };
     if (!p.dxo) {       // nothing comes from further on: the slots stay zeros
@@ -130,7 +133,7 @@ __global__ void __launch_bounds__(bwd_threads(V, 2 + SB + SA), 1) k_norm_bwd(con
                 asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(base + k * Ring::kStage + at16 + i * N * 16), "r"(0) : "memory");
     }
 #pragma unroll
-    for (int k = 0; k < S - 1; k++) fetch(first + k, base + k * Ring::kStage);
+    for (int k = 0; k < S - 1; k++) fetch(first + k * step, base + k * Ring::kStage);
     pm = pr = qm = qr = 0.0f;
 #pragma unroll
     for (int i = 0; i < V; i++) xs[i] = fs[i] = 0;
@@ -186,13 +189,13 @@ __global__ void __launch_bounds__(bwd_threads(V, 2 + SB + SA), 1) k_norm_bwd(con
     uint32_t slot = 0;
     XT *dx = static_cast<XT *>(p.dx) + first * p.lddx + t.first_vec * 8;       // the lane's places in this row
     __nv_bfloat16 *df = p.df + first * p.lddf + t.first_vec * 8;
-    const int turns = L < 32 ? (int)p.rows_per_team : (int)(end - first);
-    for (int k = 0; k < turns; k++, dx += p.lddx, df += p.lddf) {
-        const int64_t row = first + k;
+    const int turns = L < 32 ? (int)p.rows_per_team : first < end ? (int)((end - first + step - 1) / step) : 0;
+    for (int k = 0; k < turns; k++, dx += step * p.lddx, df += step * p.lddf) {
+        const int64_t row = first + k * step;
         const bool live = EXACT || row < end;
         const int n = live ? have : 0;
         if (sizeof(XT) == 4) warp_sync();      // the others have read what is overwritten
-        fetch(row + S - 1, base + (slot == 0 ? S - 1 : slot - 1) * Ring::kStage);
+        fetch(row + (S - 1) * step, base + (slot == 0 ? S - 1 : slot - 1) * Ring::kStage);
         const uint32_t stage = base + slot * Ring::kStage;
         slot = slot == S - 1 ? 0 : slot + 1;
         if (NEED_F && p.several && live) {
@@ -207,7 +210,7 @@ __global__ void __launch_bounds__(bwd_threads(V, 2 + SB + SA), 1) k_norm_bwd(con
         float xsc[V], fsc[V];
 #pragma unroll
         for (int i = 0; i < V; i++) xsc[i] = ckpt_scale(xs[i]), fsc[i] = ckpt_scale(fs[i]);
-        fetch_small(row + 1);
+        fetch_small(row + step);
         async_wait<S - 1>();
         if (sizeof(XT) == 4) warp_sync();
         f2 xh[V][4], d[V][4];

@@ -15,6 +15,7 @@ struct NormFwd {
     int64_t ldg;
     uint32_t rows_per_gate;
     int gate_fp32, several;     // several gates
+    int gate_in_ring;
     int has_cw, has_cb;         // f^ has a factor other than s, a summand
     int stages;                 // of the ring
     int wide;                   // x' in FP32 lies on 32 bytes
@@ -101,13 +102,14 @@ __device__ __forceinline__ bool row_ckpt(const CkptOut &o, const Team<L> &t, int
 template <class XT, int V, bool HAS_F> struct FwdRing {
     static constexpr int N = kFwdThreads;
     static constexpr int kF = kSlots<XT> * V * N * 16;                        // where f starts in a stage
-    static constexpr int kStage = kF + (HAS_F ? V * N * 16 : 0);
+    static constexpr int kG = kF + (HAS_F ? V * N * 16 : 0);                  // and, of several gates, the row's gate where there is room for it
+    static constexpr int gate_bytes(bool fp32) { return V * N * (fp32 ? 32 : 16); }
 };
 
 // x' = a x + (f^ cw + cb) [g], h = x^ pw + pb; cw = s w1 and cb = s b1, with one gate s g w1 and s g b1: the block keeps them in shared
 // memory as far as there are any (in registers they would leave room for eight warps instead of sixteen).
 template <class XT, int L, int V, bool FULL, bool HAS_F, bool POST, bool PRE>
-__global__ void __launch_bounds__(kFwdThreads, 1) k_norm_fwd(const __grid_constant__ NormFwd p)
+__global__ void __launch_bounds__(kFwdThreads, 2) k_norm_fwd(const __grid_constant__ NormFwd p)
 {
     using Ring = FwdRing<XT, V, HAS_F>;
     constexpr int N = kFwdThreads;
@@ -116,17 +118,18 @@ __global__ void __launch_bounds__(kFwdThreads, 1) k_norm_fwd(const __grid_consta
     pdl_launch_dependents();
     Team<L> t(p.warps, V, s_sum);
     const int64_t team = (int64_t)blockIdx.x * p.teams + t.id;
-    // rows first, first + step, ...: all teams side by side (what they read at a time lies together: 401408 x 96 in runs of rows 98 us, so
-    // 74), with several gates the block's teams in a run of rows, which share the gate
-    const int64_t run = (int64_t)blockIdx.x * p.teams * p.rows_per_team, end = p.several ? min(run + p.teams * p.rows_per_team, p.rows) : p.rows;
-    const int64_t step = p.several ? p.teams : (int64_t)gridDim.x * p.teams, first = t.id < p.teams ? (p.several ? run + t.id : team) : p.rows;
+    // rows first, first + step, ...: what is read at a time lies side by side (401408 x 96: 73 us, with a run of rows for each team 98); where
+    // gates come by way of L1 the block has a run of rows, for its teams to share them
+    const bool runs = HAS_F && p.several && !p.gate_in_ring;
+    const int64_t run = runs ? (int64_t)blockIdx.x * p.teams * p.rows_per_team : 0, end = runs ? min(run + p.teams * p.rows_per_team, p.rows) : p.rows;
+    const int64_t step = runs ? p.teams : (int64_t)gridDim.x * p.teams, first = t.id < p.teams ? (runs ? run + t.id : team) : p.rows;
     constexpr bool EXACT = FULL && L == 32;      // each turn of each lane has a row and all of its vectors
     const int have = FULL ? V : max(0, min(V, (p.nvec - t.first_vec + L - 1) / L));   // vectors of this lane
     const int lanes = p.nvec - t.first_vec + t.lane;     // vectors of the row from this part's first lane on
     const float inv = 1.0f / (float)p.cols;
-    const int S = p.stages;
+    const int S = p.stages, stage_bytes = Ring::kG + (p.gate_in_ring ? Ring::gate_bytes(p.gate_fp32) : 0);
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(s_ring);
-    float4 *const plane_cw = reinterpret_cast<float4 *>(s_ring + S * Ring::kStage), *const plane_cb = plane_cw + (p.has_cw ? 2 * p.nvec : 0);
+    float4 *const plane_cw = reinterpret_cast<float4 *>(s_ring + S * stage_bytes), *const plane_cb = plane_cw + (p.has_cw ? 2 * p.nvec : 0);
     float4 *const plane_pw = plane_cb + (p.has_cb ? 2 * p.nvec : 0), *const plane_pb = plane_pw + (p.pre.w ? 2 * p.nvec : 0);
     pdl_wait();
 
@@ -144,10 +147,18 @@ __global__ void __launch_bounds__(kFwdThreads, 1) k_norm_fwd(const __grid_consta
                 fp += step * p.ldf;
             }
             xp += step * p.ldx;
+            if (HAS_F && p.gate_in_ring) {
+                const int64_t g = (int64_t)((uint32_t)row / p.rows_per_gate) * p.ldg + t.first_vec * 8;
+#pragma unroll
+                for (int i = 0; i < V; i++) {
+                    if (p.gate_fp32) async_row8<float, L>(stage + Ring::kG + i * N * 32, static_cast<const float *>(p.gate) + g + i * L * 8, FULL ? L : lanes - i * L);
+                    else async_row8<__nv_bfloat16, L>(stage + Ring::kG + i * N * 16, static_cast<const __nv_bfloat16 *>(p.gate) + g + i * L * 8, FULL ? L : lanes - i * L);
+                }
+            }
         }
         async_commit();
     };
-    for (int k = 0; k < S - 1; k++) fetch(first + k * step, ring + k * Ring::kStage);
+    for (int k = 0; k < S - 1; k++) fetch(first + k * step, ring + k * stage_bytes);
 
     for (int vec = threadIdx.x; vec < p.nvec; vec += N) {
         f2 w[4], b[4];
@@ -182,13 +193,13 @@ __global__ void __launch_bounds__(kFwdThreads, 1) k_norm_fwd(const __grid_consta
     for (int k = 0; k < turns; k++) {
         const int64_t row = first + k * step;
         const bool live = EXACT || row < end;
-        if (sizeof(XT) == 4) warp_sync();      // the others have read what is overwritten
-        fetch(row + (S - 1) * step, ring + (slot == 0 ? S - 1 : slot - 1) * Ring::kStage);
-        const uint32_t stage = ring + slot * Ring::kStage;
+        if (sizeof(XT) == 4 || (HAS_F && p.gate_in_ring)) warp_sync();      // the others have read what is overwritten
+        fetch(row + (S - 1) * step, ring + (slot == 0 ? S - 1 : slot - 1) * stage_bytes);
+        const uint32_t stage = ring + slot * stage_bytes;
         slot = slot == S - 1 ? 0 : slot + 1;
         const int n = live ? have : 0;
         async_wait_all_but(S - 1);
-        if (sizeof(XT) == 4) warp_sync();
+        if (sizeof(XT) == 4 || (HAS_F && p.gate_in_ring)) warp_sync();
         f2 v[V][4];
         float r = 1.0f;
         if (HAS_F) {
@@ -223,13 +234,15 @@ __global__ void __launch_bounds__(kFwdThreads, 1) k_norm_fwd(const __grid_consta
                     }
                 }
                 if (p.has_cb) r = 1.0f;
-                if (p.several && live) {
-                    const int64_t gate = (uint32_t)row / p.rows_per_gate;
+                if (p.several) {
+                    const int64_t gate = live ? (int64_t)((uint32_t)row / p.rows_per_gate) * p.ldg + t.first_vec * 8 : 0;
 #pragma unroll
                     for (int i = 0; i < V; i++) {
                         f2 g[4];
-                        if (FULL || i < have) load_param8(p.gate, p.gate_fp32, gate * p.ldg + (i * L + t.first_vec) * 8, g);
-                        else zero8(g);
+                        if (!(EXACT || i < n)) zero8(g);
+                        else if (!p.gate_in_ring) load_param8(p.gate, p.gate_fp32, gate + i * L * 8, g);
+                        else if (p.gate_fp32) ring_row8<float>(stage + Ring::kG + i * N * 32, g);
+                        else ring_row8<__nv_bfloat16>(stage + Ring::kG + i * N * 16, g);
 #pragma unroll
                         for (int j = 0; j < 4; j++) v[i][j] = f2_mul(v[i][j], g[j]);
                     }
@@ -340,8 +353,16 @@ template <class XT> cudaError_t launch_norm_fwd(NormFwd &p, const RowPlan &plan,
                 return cudaErrorInvalidValue;     // refused by the caller
             } else {
                 const size_t planes = (size_t)(p.has_cw + p.has_cb + (R && p.pre.w) + (R && p.pre.b)) * p.cols * 4;
-                p.stages = ring_stages(planes, FwdRing<XT, V, F>::kStage);      // one at least: 128 KB of planes and 96 KB
-                return launch_ring<k_norm_fwd<XT, L, V, decltype(full)::value, F, Q, R>, kFwdThreads>(plan.blocks, p.stages * FwdRing<XT, V, F>::kStage + planes, st, p);
+                // two stages in half of an SM's shared memory, or as many as there is room for in all of it (one at least: 128 KB of planes
+                // and 48 KB).  The row's gate travels with them if that does not take the second block's place (50432 x 1024 in FP32: 144 us
+                // with it and one block per SM, 127 with two and the gate by way of L1)
+                using Ring = FwdRing<XT, V, F>;
+                const auto fits = [&](size_t stage) { return planes + 2 * stage <= kHalfRingBytes; };
+                const size_t gate = p.several ? Ring::gate_bytes(p.gate_fp32) : 0;
+                p.gate_in_ring = p.several && fits(Ring::kG + gate);
+                const size_t stage = Ring::kG + (p.gate_in_ring ? gate : 0), room = fits(stage) ? kHalfRingBytes : kRingBytes;
+                p.stages = (int)std::min<size_t>((room - planes) / stage, kMostStages);
+                return launch_ring<k_norm_fwd<XT, L, V, decltype(full)::value, F, Q, R>, kFwdThreads>(plan.blocks, p.stages * stage + planes, st, p);
             }
         });
     };
