@@ -62,6 +62,7 @@ __global__ void __launch_bounds__(bwd_threads(V, 2 + SB + SA), bwd_blocks_per_sm
     using Ring = BwdRing<XT, V, 2 + SB + SA, EIGHT, NEED_F, PRE>;
     constexpr int N = Ring::N, S = Ring::kDepth;
     __shared__ float4 s_sum[2 * (N / 32)];
+    __shared__ uint2 s_gates[N / L < N / 32 ? N / 32 : N / L];     // each team's first and last gate
     extern __shared__ __align__(128) uint8_t s_ring[];
     pdl_launch_dependents();
     Team<L> t(p.warps, V, s_sum);
@@ -126,6 +127,33 @@ __global__ void __launch_bounds__(bwd_threads(V, 2 + SB + SA), bwd_blocks_per_sm
             xs_at += step * (p.cols >> 5), fs_at += step * (p.cols >> 5);
         }
     };
+    uint32_t gate = p.several ? (uint32_t)first / p.rows_per_gate : 0u;
+    uint32_t left = p.several ? p.rows_per_gate - ((uint32_t)first - gate * p.rows_per_gate) : 0u;   // rows of this gate still to come
+    pm = pr = qm = qr = 0.0f;
+#pragma unroll
+    for (int i = 0; i < V; i++) xs[i] = fs[i] = 0;
+    // the parameters' loads go first: behind the rows' they would wait for all of them (2 us), and one after the other for each other
+    f2 w1[V][4], w2[V][4], wg[V][4], none[4];
+    const auto get_gate = [&](int64_t gate) {
+#pragma unroll
+        for (int i = 0; i < V; i++) {
+            zero8(w2[i]), zero8(wg[i]);
+            if (i < have) {
+                const int vec = i * L + t.first_vec;
+                load_side8({POST ? p.post.w : nullptr, nullptr, p.post.fp32, 0, 0.0f}, vec, w2[i], none);
+                if (p.gate) load_param8(p.gate, p.gate_fp32, gate * p.ldg + vec * 8, wg[i]);
+            }
+        }
+    };
+    if (PRE) {
+#pragma unroll
+        for (int i = 0; i < V; i++) {
+            zero8(w1[i]);
+            if (i < have) load_side8({p.pre.w, nullptr, p.pre.fp32, 0, 0.0f}, i * L + t.first_vec, w1[i], none);
+        }
+    }
+    if (NEED_F) get_gate(first < end ? gate : 0);
+    fetch_small(first);
     if (!p.dxo) {       // nothing comes from further on: the slots stay zeros
         for (int k = 0; k < S; k++)
 #pragma unroll
@@ -134,45 +162,25 @@ __global__ void __launch_bounds__(bwd_threads(V, 2 + SB + SA), bwd_blocks_per_sm
     }
 #pragma unroll
     for (int k = 0; k < S - 1; k++) fetch(first + k * step, base + k * Ring::kStage);
-    pm = pr = qm = qr = 0.0f;
-#pragma unroll
-    for (int i = 0; i < V; i++) xs[i] = fs[i] = 0;
-    fetch_small(first);
 
     const uint32_t w_at = base + S * Ring::kStage + at16, g_at = w_at + Ring::kW;
     if (PRE) {
 #pragma unroll
-        for (int i = 0; i < V; i++) {
-            f2 w[4], none[4];
-            zero8(w);
-            if (i < have) load_side8({p.pre.w, nullptr, p.pre.fp32, 0, 0.0f}, i * L + t.first_vec, w, none);
-            sts8<N>(w_at + i * N * 32, w);
-        }
+        for (int i = 0; i < V; i++) sts8<N>(w_at + i * N * 32, w1[i]);
     }
-    const auto new_gate = [&](int64_t gate) {
+    const auto put_gate = [&]() {
 #pragma unroll
         for (int i = 0; i < V; i++) {
-            f2 w[4], g[4];
-            zero8(w);
-            if (i < have) {
-                const int vec = i * L + t.first_vec;
-                load_side8({POST ? p.post.w : nullptr, nullptr, p.post.fp32, 0, 0.0f}, vec, w, g);
 #pragma unroll
-                for (int j = 0; j < 4; j++) g[j] = f2_of(1.0f, 1.0f);
-                if (p.gate) load_param8(p.gate, p.gate_fp32, gate * p.ldg + vec * 8, g);
-#pragma unroll
-                for (int j = 0; j < 4; j++) w[j] = f2_mul(w[j], f2_mul(g[j], f2_of(p.s, p.s)));
-            }
-            sts8<N>(g_at + i * N * 32, w);
+            for (int j = 0; j < 4; j++) w2[i][j] = f2_mul(w2[i][j], f2_mul(p.gate ? wg[i][j] : f2_of(1.0f, 1.0f), f2_of(p.s, p.s)));
+            sts8<N>(g_at + i * N * 32, w2[i]);
         }
     };
 
     f2 sw[V][4], sb[V][4], B[V][4], A[V][4];
 #pragma unroll
     for (int i = 0; i < V; i++) zero8(sw[i]), zero8(sb[i]), zero8(B[i]), zero8(A[i]);
-    uint32_t gate = p.several ? (uint32_t)first / p.rows_per_gate : 0u;
-    uint32_t left = p.several ? p.rows_per_gate - ((uint32_t)first - gate * p.rows_per_gate) : 0u;   // rows of this gate still to come
-    if (NEED_F && first < end) new_gate(gate);
+    if (NEED_F) put_gate();
     const uint32_t first_gate = gate;
     const auto flush = [&]() {     // the rows of a gate are done and the team goes on: its first one is left to the block's end, any other is whole
         float *o = gate == first_gate ? p.heads + team * 2 * p.cols : p.slots + ((int64_t)blockIdx.x + gate) * 2 * p.cols;
@@ -201,7 +209,8 @@ __global__ void __launch_bounds__(bwd_threads(V, 2 + SB + SA), bwd_blocks_per_sm
         if (NEED_F && p.several && live) {
             if (left == 0) {
                 flush();
-                new_gate(++gate);
+                get_gate(++gate);
+                put_gate();
                 left = p.rows_per_gate;
             }
             left--;
@@ -358,6 +367,7 @@ __global__ void __launch_bounds__(bwd_threads(V, 2 + SB + SA), bwd_blocks_per_sm
     if (with_f && SA) leave(A, 3);
     float *const last = reinterpret_cast<float *>(s_ring) + (int64_t)parts * 4 * cols;     // [team][2][cols]: of each team's last gate
     if (NEED_F && p.several) {
+        if (t.leader) s_gates[t.id] = make_uint2(first_gate, gate);
 #pragma unroll
         for (int i = 0; i < V; i++)
             if ((FULL || i < have) && in_team) {
@@ -381,9 +391,10 @@ __global__ void __launch_bounds__(bwd_threads(V, 2 + SB + SA), bwd_blocks_per_sm
     if (NEED_F && p.several) {
         // along the block's teams: what they have of one gate follows each other, a team's first gate, (gates that are its own,) its last
         const int64_t row0 = (int64_t)blockIdx.x * p.teams * p.rows_per_team;
+        const int with_rows = (int)min((int64_t)p.teams, (p.rows - row0 + p.rows_per_team - 1) / p.rows_per_team);
         for (int c = threadIdx.x * 4; c < 2 * cols; c += N * 4) {
             float4 v = make_float4(0, 0, 0, 0);
-            uint32_t now = (uint32_t)row0 / p.rows_per_gate;
+            uint32_t now = s_gates[0].x;
             const auto add = [&](const float *at) {
                 const float4 w = *reinterpret_cast<const float4 *>(at + c);
                 v.x += w.x, v.y += w.y, v.z += w.z, v.w += w.w;
@@ -393,10 +404,8 @@ __global__ void __launch_bounds__(bwd_threads(V, 2 + SB + SA), bwd_blocks_per_sm
                 v = make_float4(0, 0, 0, 0);
                 now = next;
             };
-            for (int k = 0; k < p.teams; k++) {
-                const int64_t from = row0 + k * p.rows_per_team, to = min(from + p.rows_per_team, p.rows);
-                if (from >= to) break;
-                const uint32_t a = (uint32_t)from / p.rows_per_gate, b = (uint32_t)(to - 1) / p.rows_per_gate;
+            for (int k = 0; k < with_rows; k++) {
+                const uint32_t a = s_gates[k].x, b = s_gates[k].y;
                 if (a != now) put(a);
                 if (b != a) add(p.heads + ((int64_t)blockIdx.x * p.teams + k) * 2 * cols), put(b);
                 add(last + (int64_t)k * 2 * cols);

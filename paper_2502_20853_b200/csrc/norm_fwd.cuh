@@ -158,28 +158,30 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_norm_fwd(const __grid_consta
         }
         async_commit();
     };
+    // the parameters' loads go first: behind the rows' they would wait for all of them (2 us)
+    f2 pw[4], pb[4], cw[4], cb[4], g[4];
+    const auto get_params = [&](int vec) {
+        if (PRE) load_side8(p.pre, vec, pw, pb);
+        if (HAS_F && p.has_cw) load_side8(POST ? p.post : NormSide{}, vec, cw, cb);
+#pragma unroll
+        for (int j = 0; j < 4; j++) g[j] = f2_of(1.0f, 1.0f);
+        if (HAS_F && p.gate && !p.several) load_param8(p.gate, p.gate_fp32, vec * 8, g);
+    };
+    if (threadIdx.x < p.nvec) get_params(threadIdx.x);
     for (int k = 0; k < S - 1; k++) fetch(first + k * step, ring + k * stage_bytes);
 
     for (int vec = threadIdx.x; vec < p.nvec; vec += N) {
-        f2 w[4], b[4];
-        if (PRE) {
-            load_side8(p.pre, vec, w, b);
-            if (p.pre.w) plane_put(plane_pw, p.nvec, vec, w);
-            if (p.pre.b) plane_put(plane_pb, p.nvec, vec, b);
-        }
+        if (vec >= N) get_params(vec);
+        if (PRE && p.pre.w) plane_put(plane_pw, p.nvec, vec, pw);
+        if (PRE && p.pre.b) plane_put(plane_pb, p.nvec, vec, pb);
         if (HAS_F && p.has_cw) {
-            f2 g[4];
-            load_side8(POST ? p.post : NormSide{}, vec, w, b);
-#pragma unroll
-            for (int j = 0; j < 4; j++) g[j] = f2_of(1.0f, 1.0f);
-            if (p.gate && !p.several) load_param8(p.gate, p.gate_fp32, vec * 8, g);
 #pragma unroll
             for (int j = 0; j < 4; j++) {
                 g[j] = f2_mul(g[j], f2_of(p.s, p.s));
-                w[j] = f2_mul(w[j], g[j]), b[j] = f2_mul(b[j], g[j]);
+                cw[j] = f2_mul(cw[j], g[j]), cb[j] = f2_mul(cb[j], g[j]);
             }
-            plane_put(plane_cw, p.nvec, vec, w);
-            if (p.has_cb) plane_put(plane_cb, p.nvec, vec, b);
+            plane_put(plane_cw, p.nvec, vec, cw);
+            if (p.has_cb) plane_put(plane_cb, p.nvec, vec, cb);
         }
     }
     __syncthreads();
