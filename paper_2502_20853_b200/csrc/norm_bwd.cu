@@ -56,21 +56,50 @@ __global__ void __launch_bounds__(256) k_norm_bwd_finish(const __grid_constant__
         const int q = threadIdx.x & 1, r = threadIdx.x >> 1, c = blockIdx.x * 8 + q * 4;
         float4 v[4] = {all4(0), all4(0), all4(0), all4(0)};     // of dh x^, dh, t f^ (with several gates times g), t (the same)
         const bool f = p.use_f && !p.several;
-        for (int k = r; k < p.blocks; k += 128) {
+        // (a lane's few blocks all at once: one after the other each would take a trip to the L2)
+        constexpr int kMost = (2 * kSms + 127) / 128;
+        const bool slots = p.use_f && p.several && (p.dw_post || p.db_post);
+        float4 part[kMost][4], w[kMost];
+        uint32_t now[kMost], last[kMost];
+#pragma unroll
+        for (int i = 0; i < kMost; i++) {
+            const int k = r + i * 128;
             const float *at = p.part + (int64_t)k * 4 * p.cols + c;
-            if (p.pre) add4(v[0], load4(at));
-            if (p.sb) add4(v[1], load4(at + p.cols));
-            if (f) add4(v[2], load4(at + 2 * p.cols));
-            if (f && p.sa) add4(v[3], load4(at + 3 * p.cols));
-        }
-        if (p.use_f && p.several && (p.dw_post || p.db_post))
-            for (int k = r; k < p.blocks; k += 128) {
+            const bool on = k < p.blocks;
+#pragma unroll
+            for (int j = 0; j < 4; j++) part[i][j] = all4(0);
+            w[i] = all4(1), now[i] = 1, last[i] = 0;
+            if (on && p.pre) part[i][0] = load4(at);
+            if (on && p.sb) part[i][1] = load4(at + p.cols);
+            if (on && f) part[i][2] = load4(at + 2 * p.cols);
+            if (on && f && p.sa) part[i][3] = load4(at + 3 * p.cols);
+            if (on && slots) {
                 const int64_t first = k * p.rows_per_block, end = first + p.rows_per_block < p.rows ? first + p.rows_per_block : p.rows;
-                for (uint32_t g = (uint32_t)first / (uint32_t)p.rows_per_gate; g <= (uint32_t)(end - 1) / (uint32_t)p.rows_per_gate; g++) {
-                    const float *at = p.slots + (int64_t)(k + g) * 2 * p.cols + c;
-                    const float4 w = param4(p.gate, p.gate_fp32, g * p.ldg + c);
-                    add4(v[2], mul4(load4(at), w)), add4(v[3], mul4(load4(at + p.cols), w));
+                now[i] = (uint32_t)first / (uint32_t)p.rows_per_gate, last[i] = (uint32_t)(end - 1) / (uint32_t)p.rows_per_gate;
+                const float *s = p.slots + (int64_t)(k + now[i]) * 2 * p.cols + c;
+                part[i][2] = load4(s);
+                if (p.sa) part[i][3] = load4(s + p.cols);
+                w[i] = param4(p.gate, p.gate_fp32, now[i] * p.ldg + c);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kMost; i++) add4(v[0], part[i][0]), add4(v[1], part[i][1]), add4(v[2], mul4(part[i][2], w[i])), add4(v[3], mul4(part[i][3], w[i]));
+        if (slots)
+            for (bool more = true; more;) {      // the next gate of each of them
+                more = false;
+#pragma unroll
+                for (int i = 0; i < kMost; i++) {
+                    part[i][2] = part[i][3] = all4(0);
+                    if (now[i]++ < last[i]) {
+                        const float *s = p.slots + (int64_t)(r + i * 128 + now[i]) * 2 * p.cols + c;
+                        part[i][2] = load4(s);
+                        if (p.sa) part[i][3] = load4(s + p.cols);
+                        w[i] = param4(p.gate, p.gate_fp32, now[i] * p.ldg + c);
+                        more = true;
+                    }
                 }
+#pragma unroll
+                for (int i = 0; i < kMost; i++) add4(v[2], mul4(part[i][2], w[i])), add4(v[3], mul4(part[i][3], w[i]));
             }
 #pragma unroll
         for (int i = 0; i < 4; i++) {
