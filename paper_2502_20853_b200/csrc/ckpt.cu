@@ -88,31 +88,30 @@ __device__ __forceinline__ f2 logistic(f2 y)
 __host__ __device__ constexpr bool act_is_gelu(int act) { return act == MXFP4_ACT_GELU || act == MXFP4_ACT_GEGLU; }
 __host__ __device__ constexpr bool act_is_gated(int act) { return act == MXFP4_ACT_GEGLU || act == MXFP4_ACT_SWIGLU; }
 
-// act(y) of a pair: GELU = max(y, 0) - |y| e (no cancellation), SiLU = y p.  +Inf gives +Inf, NaN NaN.
-template <int ACT>
-__device__ __forceinline__ f2 act_value(f2 y)
-{
-    if (!act_is_gelu(ACT)) return f2_mul(y, logistic(y));
-    float a, b, p, q;
-    f2_to(y, a, b);
-    p = a < 0.0f ? 0.0f : a, q = b < 0.0f ? 0.0f : b;             // a NaN stays
-    const f2 c = f2_of(fminf(fabsf(a), 3e38f), fminf(fabsf(b), 3e38f));
-    return f2_fma(f2_mul(c, f2_all(-0.125f)), tail8(c), f2_of(p, q));
-}
-// act'(y): GELU' = Phi(y) + y phi(y) with Phi = e or 1 - e by the sign, SiLU' = p (1 + y (1 - p))
-template <int ACT>
-__device__ __forceinline__ f2 act_slope(f2 y)
+// act(y) of a pair (VALUE) and act'(y) (SLOPE), from one logistic or one tail:
+//   GELU  max(y, 0) - |y| e (no cancellation) and Phi(y) + y phi(y) with Phi = e or 1 - e by the sign
+//   SiLU  y p and p (1 + y (1 - p))
+// +Inf gives the value +Inf, NaN NaN.
+template <int ACT, bool VALUE, bool SLOPE>
+__device__ __forceinline__ void act_pair(f2 y, f2 &value, f2 &slope)
 {
     if (!act_is_gelu(ACT)) {
         const f2 p = logistic(y);
-        return f2_mul(p, f2_fma(y, f2_fma(p, f2_all(-1.0f), f2_all(1.0f)), f2_all(1.0f)));
+        if (VALUE) value = f2_mul(y, p);
+        if (SLOPE) slope = f2_mul(p, f2_fma(y, f2_fma(p, f2_all(-1.0f), f2_all(1.0f)), f2_all(1.0f)));
+        return;
     }
-    float e0, e1, y0, y1;
-    f2_to(f2_mul(tail8(y), f2_all(0.125f)), e0, e1);
-    f2_to(y, y0, y1);
-    e0 = y0 > 0.0f ? 1.0f - e0 : e0, e1 = y1 > 0.0f ? 1.0f - e1 : e1;
-    // phi(y) = 2^(-y^2 log2(e) / 2 - log2(2 pi) / 2)
-    return f2_fma(y, f2_ex2(f2_fma(f2_mul(y, y), f2_all(-0.72134752f), f2_all(-1.32574806f))), f2_of(e0, e1));
+    float a, b;
+    f2_to(y, a, b);
+    const f2 c = f2_of(fminf(fabsf(a), 3e38f), fminf(fabsf(b), 3e38f)), e8 = tail8(c);
+    if (VALUE) value = f2_fma(f2_mul(c, f2_all(-0.125f)), e8, f2_of(a < 0.0f ? 0.0f : a, b < 0.0f ? 0.0f : b));     // a NaN stays
+    if (SLOPE) {
+        float e0, e1;
+        f2_to(f2_mul(e8, f2_all(0.125f)), e0, e1);
+        e0 = a > 0.0f ? 1.0f - e0 : e0, e1 = b > 0.0f ? 1.0f - e1 : e1;
+        // phi(y) = 2^(-y^2 log2(e) / 2 - log2(2 pi) / 2)
+        slope = f2_fma(y, f2_ex2(f2_fma(f2_mul(y, y), f2_all(-0.72134752f), f2_all(-1.32574806f))), f2_of(e0, e1));
+    }
 }
 
 template <int ACT, int U>
@@ -162,7 +161,11 @@ __global__ void __launch_bounds__(kEw) k_act_fwd(const __nv_bfloat16 *y, int64_t
             } else {
                 f2 o[4];
 #pragma unroll
-                for (int j = 0; j < 4; j++) o[j] = H == 1 ? act_value<ACT>(v[0][j]) : f2_mul(act_value<ACT>(v[0][j]), v[H - 1][j]);
+                for (int j = 0; j < 4; j++) {
+                    f2 none;
+                    act_pair<ACT, true, false>(v[0][j], o[j], none);
+                    if (H == 2) o[j] = f2_mul(o[j], v[H - 1][j]);
+                }
                 q = pack8(o);
             }
             *reinterpret_cast<uint4 *>(z + place(i, nvec, ldz)) = q;
@@ -181,12 +184,14 @@ __global__ void __launch_bounds__(kEw) k_act_bwd(const __nv_bfloat16 *dz, int64_
     const int64_t i0 = blockIdx.x * (int64_t)(kEw * U) + threadIdx.x;
     uint4 raw[U];
     RawCkpt ck[U][H];
+    int64_t row[U];      // of a gated activation
 #pragma unroll
     for (int u = 0; u < U; u++) {
         const int64_t i = i0 + u * kEw;
+        row[u] = H == 2 ? row_of(i, nvec) : 0;
         if (i < total) {
-            raw[u] = ld_stream_16(dz + place(i, nvec, lddz));
-            const int64_t at = H == 1 ? i : i + row_of(i, nvec) * nvec;
+            raw[u] = ld_stream_16(dz + (H == 2 ? row[u] * lddz + (i - row[u] * nvec) * 8 : place(i, nvec, lddz)));
+            const int64_t at = H == 1 ? i : i + row[u] * nvec;
             ck[u][0].load(codes, scales, at);
             if (H == 2) ck[u][H - 1].load(codes, scales, at + nvec);
         }
@@ -195,24 +200,20 @@ __global__ void __launch_bounds__(kEw) k_act_bwd(const __nv_bfloat16 *dz, int64_
     for (int u = 0; u < U; u++) {
         const int64_t i = i0 + u * kEw;
         if (i >= total) continue;
-        f2 d[4], a[4], b[4], o[4];
+        f2 d[4], a[4], b[4], o[4], q[4];
         unpack8(raw[u], d);
         ck[u][0].get(a);
-        if (H == 2) {
-            ck[u][H - 1].get(b);
+        if (H == 2) ck[u][H - 1].get(b);
 #pragma unroll
-            for (int j = 0; j < 4; j++) o[j] = f2_mul(d[j], act_value<ACT>(a[j])), d[j] = f2_mul(d[j], b[j]);
-            const int64_t r = row_of(i, nvec);
-            __nv_bfloat16 *p = dy + r * lddy + (i - r * nvec) * 8;
-            store8(p + nvec * 8, o);
-#pragma unroll
-            for (int j = 0; j < 4; j++) o[j] = f2_mul(d[j], act_slope<ACT>(a[j]));
-            store8(p, o);
-        } else {
-#pragma unroll
-            for (int j = 0; j < 4; j++) o[j] = f2_mul(d[j], act_slope<ACT>(a[j]));
-            store8(dy + place(i, nvec, lddy), o);
+        for (int j = 0; j < 4; j++) {
+            f2 value, slope;
+            act_pair<ACT, H == 2, true>(a[j], value, slope);
+            o[j] = f2_mul(H == 2 ? f2_mul(d[j], b[j]) : d[j], slope);
+            if (H == 2) q[j] = f2_mul(d[j], value);
         }
+        __nv_bfloat16 *p = dy + (H == 2 ? row[u] * lddy + (i - row[u] * nvec) * 8 : place(i, nvec, lddy));
+        store8(p, o);
+        if (H == 2) store8(p + nvec * 8, q);
     }
 }
 
