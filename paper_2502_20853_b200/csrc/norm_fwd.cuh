@@ -71,6 +71,7 @@ template <int V, bool FULL, int L>
 __device__ __forceinline__ bool row_ckpt(const CkptOut &o, const Team<L> &t, int n, const f2 (&v)[V][4], float r, int64_t at)
 {
     uint32_t m[V], byte[V], worst = 0;
+    bool low = false;
     uint2 c[V];
 #pragma unroll
     for (int i = 0; i < V; i++) m[i] = amax8(v[i]);
@@ -81,11 +82,19 @@ __device__ __forceinline__ bool row_ckpt(const CkptOut &o, const Team<L> &t, int
         byte[i] = ckpt_scale_byte(m[i], o.tf_add);
         c[i] = e4m3_x8(v[i], __uint_as_float((254u - byte[i]) << 23) * r);
         worst = max(worst, m[i]);
+        low |= byte[i] < 32u;
     }
-    if (worst >= 0x7F800000u) {      // a group that is not finite: aside, it costs the others one comparison
+    if (worst >= 0x7F800000u || low) {      // aside, they cost the others one comparison: a group that is not finite, and one so small that 2^-s r may overflow
 #pragma unroll
-        for (int i = 0; i < V; i++)
+        for (int i = 0; i < V; i++) {
+            if (byte[i] < 32u) {
+                f2 u[4];
+#pragma unroll
+                for (int j = 0; j < 4; j++) u[j] = f2_mul(v[i][j], f2_of(r, r));
+                c[i] = e4m3_x8(u, __uint_as_float((254u - byte[i]) << 23));
+            }
             if (m[i] >= 0x7F800000u) c[i] = make_uint2(0, 0), byte[i] = 0xFFu;
+        }
     }
     if (n > 0) {
         uint8_t *codes = o.codes + at * 8, *scales = o.scales + (at >> 2);

@@ -300,6 +300,52 @@ def test_rows_without_deviation(mx):
         assert bool((ctx.f.codes == 0).all()) and bool((ctx.f.scales == 92).all())
 
 
+@pytest.mark.parametrize("scale", [1e-30, 1e-35, 1e-38, 1e30])
+def test_rows_of_extreme_size(mx, scale):
+    """eps dominates the deviation of tiny rows: their x^ are tiny numbers, for which 2^-s / deviation leaves FP32; squares of large rows do."""
+    k = Case(mx, 9, 160, "rms", "rms", 0, F32)
+    k.x.mul_(scale)
+    k.f = (k.f.float() * scale).to(BF16)
+    if scale > 1:
+        k.x.div_(1e13), k.f.div_(1e13)      # 1e17: the squares' sum stays finite
+    k.post.weight.fill_(1.0)
+    k.post.bias = k.pre.bias = None
+    k.r_pre, k.r_post = ("rms", k.pre.weight, None), ("rms", k.post.weight, None)
+    _both_ways(k, mx.SAVE_8BIT)
+
+
+@pytest.mark.parametrize("cols,rows,gates", [(32, 400000, 1), (96, 300000, 0), (64, 250000, 1250), (128, 120000, 4), (384, 60000, 300), (768, 30000, 150), (1024, 12000, 3),
+                                             (4096, 9000, 1), (8192, 2500, 25)])
+def test_many_rows(mx, cols, rows, gates):
+    """More blocks than are resident forward, long runs of rows backward."""
+    for dtype in (BF16, F32):
+        k = Case(mx, rows, cols, "layer", "layer" if gates else None, gates, dtype)
+        _both_ways(k, mx.SAVE_8BIT if dtype == BF16 else mx.SAVE_INPUTS)
+        del k
+        torch.cuda.empty_cache()
+
+
+def test_kept_inputs_are_not_written_over(mx):
+    k = Case(mx, 8, 96, "layer", "rms", 1)
+    with pytest.raises(AssertionError):
+        k.fwd(save=mx.SAVE_INPUTS, h=k.f)
+    with pytest.raises(AssertionError):
+        k.fwd(save=mx.SAVE_INPUTS, x_out=k.f)
+    with pytest.raises(AssertionError):
+        mx.residual_norm_bwd(None, None, k.fwd()[2])
+    for bad in (k.x.cpu(), k.x.double(), k.x[0], k.x.t()):
+        with pytest.raises((AssertionError, mx.MxError, ValueError)):
+            mx.residual_norm_fwd(bad, pre=k.pre)
+    with pytest.raises(AssertionError):
+        mx.residual_norm_fwd(k.x, pre=mx.Norm(mx.NORM_LAYER, k.pre.weight[:32], None))
+    with pytest.raises(AssertionError):
+        mx.residual_norm_fwd(k.x, pre=mx.Norm(mx.NORM_LAYER, k.pre.weight, k.pre.bias.to(BF16)))
+    with pytest.raises(AssertionError):
+        mx.residual_norm_fwd(k.x, k.f[:4], pre=k.pre)
+    with pytest.raises(AssertionError):
+        mx.checkpoint_load(mx.checkpoint_store(k.x), out=torch.empty(8, 64, dtype=BF16, device="cuda"))
+
+
 def test_outputs_over_inputs(mx):
     k = Case(mx, 90, 384, "layer", "rms", 3)
     x_out, h, ctx = k.fwd()
