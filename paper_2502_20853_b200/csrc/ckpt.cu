@@ -218,10 +218,9 @@ __global__ void __launch_bounds__(kEw) k_act_bwd(const __nv_bfloat16 *dz, int64_
 }
 
 // An output may lie over an input exactly (a thread writes where it has read), or not at all.
-static bool over_or_apart(const void *out, int64_t ldo, const void *in, int64_t ldi, int64_t rows, int64_t cols, bool exact_allowed)
+static bool over_or_apart(const void *out, int64_t ldo, int64_t out_cols, const void *in, int64_t ldi, int64_t in_cols, int64_t rows)
 {
-    const Span a = span_of_rows(out, ldo, rows, cols, 2), b = span_of_rows(in, ldi, rows, cols, 2);
-    return !meet(a, b) || (exact_allowed && out == in && ldo == ldi);
+    return !meet(span_of_rows(out, ldo, rows, out_cols, 2), span_of_rows(in, ldi, rows, in_cols, 2)) || (out_cols == in_cols && out == in && ldo == ldi);
 }
 static mxfp4_status_t blocks_of(int64_t total, int per_thread, unsigned *blocks)
 {
@@ -290,7 +289,7 @@ mxfp4_status_t mxfp4_act_fwd(const void *y_bf16, int64_t ldy, int64_t rows, int6
     if ((s = check_rows(y_bf16, ldy, ycols, MXFP4_OUT_BF16))) return s;
     if (z_bf16 && (s = check_rows(z_bf16, ldz, cols, MXFP4_OUT_BF16))) return s;
     if (ckpt.codes && (s = check_ckpt(ckpt, rows, ycols))) return s;
-    if (z_bf16 && !over_or_apart(z_bf16, ldz, y_bf16, ldy, rows, ycols, !gated)) return MXFP4_INVALID_ARG;
+    if (z_bf16 && !over_or_apart(z_bf16, ldz, cols, y_bf16, ldy, ycols, rows)) return MXFP4_INVALID_ARG;
     const int64_t nvec = cols / 8, total = rows * nvec;
     const CkptOut out = {ckpt.codes, ckpt.scales, ckpt_tf_add(scale_mode)};
     unsigned blocks;
@@ -313,7 +312,7 @@ mxfp4_status_t mxfp4_act_bwd(const void *dz_bf16, int64_t lddz, mxfp4_ckpt_t ckp
     if (rows == 0 || cols == 0) return MXFP4_OK;
     mxfp4_status_t s;
     if ((s = check_rows(dz_bf16, lddz, cols, MXFP4_OUT_BF16)) || (s = check_rows(dy_bf16, lddy, ckpt.cols, MXFP4_OUT_BF16)) || (s = check_ckpt(ckpt, rows, ckpt.cols))) return s;
-    if (!over_or_apart(dy_bf16, lddy, dz_bf16, lddz, rows, ckpt.cols, !gated)) return MXFP4_INVALID_ARG;
+    if (!over_or_apart(dy_bf16, lddy, ckpt.cols, dz_bf16, lddz, cols, rows)) return MXFP4_INVALID_ARG;
     const int64_t nvec = cols / 8, total = rows * nvec;
     unsigned blocks;
     if ((s = blocks_of(total, 2, &blocks))) return s;

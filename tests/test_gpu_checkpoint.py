@@ -173,6 +173,25 @@ def test_act_over_its_input(mx):
     assert torch.equal(dz, dy)
 
 
+@pytest.mark.parametrize("name", NAMES)
+def test_side_by_side(mx, name):
+    """Inputs and outputs one right behind the other in memory, in either order."""
+    half = 2 if name in ("geglu", "swiglu") else 1
+    rows, cols = 6, 64
+    buf = torch.randn(rows * cols * (2 * half + 1), device="cuda").to(BF16)
+    for first in (True, False):
+        n, k = rows * cols * half, rows * cols
+        y = (buf[:n] if first else buf[k:k + n]).view(rows, cols * half)
+        z = (buf[n:n + k] if first else buf[:k]).view(rows, cols)
+        want, c = mx.act_fwd(y.clone(), _act(mx, name))
+        mx.act_fwd(y, _act(mx, name), out=z)
+        assert torch.equal(z, want)
+        dz, dy = z, y
+        g = mx.act_bwd(dz.clone(), c, _act(mx, name))
+        mx.act_bwd(dz, c, _act(mx, name), out=dy)
+        assert torch.equal(dy, g)
+
+
 def test_no_rows(mx):
     y = torch.empty(0, 64, dtype=BF16, device="cuda")
     z, c = mx.act_fwd(y)

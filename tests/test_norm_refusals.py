@@ -50,6 +50,15 @@ def test_act_bwd(want, kw):
     assert mx.lib().mxfp4_act_bwd(a["dz"], a["lddz"], a["c"], a["act"], a["dy"], a["lddy"], None) == want
 
 
+def test_what_lies_side_by_side_does_not_overlap():
+    """Refusals of overlaps go by the bytes that each matrix has: the one argument that is wrong here is found behind them."""
+    L = mx.lib()
+    dz, dy = AT, AT + 4 * 32 * 2                  # gated: dz [4, 32], dy [4, 64] right behind it; the checkpoint's codes lie on 8 bytes
+    late = ckpt(codes=AT + (1 << 30) + 8)
+    assert L.mxfp4_act_bwd(dz, 32, late, 3, dy, 64, None) == MISALIGNED
+    assert L.mxfp4_act_bwd(dz, 32, ckpt(), 3, dy - 16, 64, None) == INVALID
+
+
 def norm(kind=1, dtype=1, weight=AT, bias=AT + (1 << 12), eps=1e-6):
     return b.CNorm(kind, dtype, weight, bias, eps, 0)
 
