@@ -9,8 +9,8 @@
 // lanes keep their columns from row to row: what belongs to a column (weights, a gate, sums over rows) is fetched once.  The few warps
 // cannot hide the memory's latency by themselves; a lane's share of the next rows travels into shared memory meanwhile (cp.async, mostly
 // into slots that only this lane reads: no barriers of the block).
-// FULL: T V vectors are exactly a row.  The kernels are bound by the instructions they issue, and without the masks of a partly filled
-// lane the loops over V are straight code.
+// FULL: the lanes' vectors are exactly a row.  Without the masks of a partly filled lane the loops over V are straight code (25216 x 384
+// forward: 343 warp instructions per 256 columns with them, 213 without).
 #pragma once
 #include <algorithm>
 

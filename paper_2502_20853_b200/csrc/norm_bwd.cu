@@ -46,6 +46,7 @@ __device__ __forceinline__ float4 gate_gradient(const NormBwdFinish &p, int c, c
 
 // Adds up what the blocks and teams have left, in a fixed order.  Two kinds of blocks: the first cols / 8 take 8 columns each, 2 lanes of
 // 4 columns by 128 lanes of rows, for the sums over all rows; then, where there are several gates, one for each gate and 128 columns.
+// 3 to 5 us with the launch, of which 1.5 pass before the other kernel's results are visible.
 __global__ void __launch_bounds__(256) k_norm_bwd_finish(const __grid_constant__ NormBwdFinish p)
 {
     __shared__ float4 s_v[8][4][2], s_g[8][2][32];

@@ -1,4 +1,9 @@
 // Residual addition between two norms, backward: the kernel that goes over the rows.
+//     t = dx' + r2 (d - mean d - x^ mean(d x^)), d = w2 dh;  dx = a t;  df = r1 (v - mean v - f^ mean(v f^)), v = s g w1 t
+// One read of dh, dx', x^ and f^, one write of dx and df; two sums over each row's lanes at a time, and the sums over rows in registers.  With one
+// norm it runs at 0.81 to 0.94 of the copy rate (50432 x 768 with biases 73 us, 50432 x 1024 RMS 76), with norms on both sides at 0.76 to 0.83 (50432 x
+// 1024 layer norms 104 us in bf16, 134 in FP32): the second sum of a row waits for the first, and the registers that hold the sums over rows
+// leave eight to sixteen warps per SM.  Rows of more than 6144 columns have one team per block (6000 x 8192: 116 us, 0.65).
 #pragma once
 #include "norm.cuh"
 
@@ -51,10 +56,10 @@ template <int N> __device__ __forceinline__ void sts8(uint32_t slot, const f2 (&
     asm volatile("st.shared.v2.u64 [%0], {%1, %2};" ::"r"(slot + N * 16), "l"(v[2]), "l"(v[3]) : "memory");
 }
 
-// Each team takes a run of consecutive rows and keeps the sums over them of its lanes' columns in registers: of dh x^ and dh for N_pre's
+// Each team keeps the sums over its rows of its lanes' columns in registers: of dh x^ and dh for N_pre's
 // gradients, and of t f^ and t (t the gradient of x' in all) for those of N_post and the gate:  with g constant over the rows of a gate,
 //     dg = s (w1 B + b1 A),   dw1 = s sum_g g B_g,   db1 = s sum_g g A_g,      B = sum t f^,  A = sum t.
-// They go to memory once per block, A and B of several gates once per block and gate; k_norm_bwd_finish adds them up. 
+// They go to memory once per block, A and B of several gates once per block and gate; k_norm_bwd_finish adds them up.
 // SB, SA: the sums of dh and of t are wanted.
 template <class XT, int L, int V, bool FULL, bool EIGHT, bool NEED_F, bool POST, bool PRE, bool SB, bool SA>
 __global__ void __launch_bounds__(bwd_threads(V, 2 + SB + SA), bwd_blocks_per_sm(V)) k_norm_bwd(const __grid_constant__ NormBwd p)

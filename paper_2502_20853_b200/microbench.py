@@ -6,7 +6,8 @@
 Kernels: quantize, quantize_sr, quantize_t, quantize_t_sr, quantize_2axis, quantize_chain, requant (double quantization), qema,
 qema_osc, qramp_detect, qramp_adamw (all elements update every step), qramp_adamw_ramped (a tenth of the elements
 accumulate over 6 steps), quant_conf_hist, change_sums, mma_ceiling (MMA-only loop, --n = tile width), gemm, linear_fwd,
-gemm_quant_gelu_chain, gemm_quant_mul_2axis, gemm_quant_chain.  Prints one line with the mean time and the algorithmic GB/s or TFLOP/s.
+gemm_quant_gelu_chain, gemm_quant_mul_2axis, gemm_quant_chain; residual_norm_fwd, residual_norm_bwd (layer norms on both sides of the branch, a
+layer scale, 8-bit checkpoints; --out fp32: an FP32 residual), act_fwd, act_bwd (GELU with its checkpoint), checkpoint_store, checkpoint_load.  Prints one line with the mean time and the algorithmic GB/s or TFLOP/s.
 """
 import argparse
 
@@ -80,6 +81,24 @@ def main():
         fn = lambda: mx.gemm(A, B, out_dtype=od, out=out, workspace=ws, dev_status=st)  # noqa: E731
         nbytes = Q * a.k * (a.m + a.n) + out.element_size() * a.m * a.n
         flops = 2.0 * a.m * a.n * a.k
+    elif a.kernel in ("residual_norm_fwd", "residual_norm_bwd"):
+        xt = torch.float32 if a.out == "fp32" else torch.bfloat16
+        rnd = lambda *s: torch.randn(*s, device="cuda")  # noqa: E731
+        x, f, gate = rnd(R, C).to(xt), rnd(R, C).to(torch.bfloat16), rnd(C) * 0.1
+        pre, post = (mx.Norm(mx.NORM_LAYER, 1 + 0.1 * rnd(C), 0.1 * rnd(C)) for _ in range(2))
+        ctx = mx.residual_norm_fwd(x, f, pre=pre, post=post, gate=gate)[2]
+        if a.kernel == "residual_norm_fwd":
+            fn = lambda: mx.residual_norm_fwd(x, f, pre=pre, post=post, gate=gate)  # noqa: E731
+        else:
+            dh, dx_out = rnd(R, C).to(torch.bfloat16), rnd(R, C).to(xt)
+            fn = lambda: mx.residual_norm_bwd(dh, dx_out, ctx)  # noqa: E731
+        nbytes = R * C * (2 * x.element_size() + 4 + 2 * (1 + 1 / 32.0))
+    elif a.kernel in ("act_fwd", "act_bwd", "checkpoint_store", "checkpoint_load"):
+        y, dz = (torch.randn(R, C, device="cuda").to(torch.bfloat16) for _ in range(2))
+        c = mx.checkpoint_store(y)
+        fn = {"act_fwd": lambda: mx.act_fwd(y), "act_bwd": lambda: mx.act_bwd(dz, c), "checkpoint_store": lambda: mx.checkpoint_store(y, out=c),
+              "checkpoint_load": lambda: mx.checkpoint_load(c)}[a.kernel]
+        nbytes = R * C * ((4 if a.kernel.startswith("act") else 2) + 1 + 1 / 32.0)
     else:
         x = torch.randn(R, C, device="cuda", dtype=torch.bfloat16)
         q, qt = mx.QMat(R, C), mx.QMat(C, R)
