@@ -161,6 +161,33 @@ def test_act_against_differences(mx):
     assert float((slope - (up.float() - down.float()) / (2 * step)).abs().max()) <= 2 * 2 * 2.0 ** -8 * 3.25 + 1.2 * step * step / 6 + 2.0 ** -7
 
 
+def test_gelu_is_the_epilogues(mx):
+    """Between two layers GELU may be the product's epilogue or a pass of its own: the same bits."""
+    g = torch.Generator(device="cuda").manual_seed(2)
+    a, b = (mx.quantize(torch.randn(n, 96, device="cuda", generator=g).to(BF16)) for n in (160, 224))
+    y, z = torch.empty(160, 224, dtype=BF16, device="cuda"), torch.empty(160, 224, dtype=BF16, device="cuda")
+    mx.gemm_quant(a, b, mx.Epilogue(hook=mx.HOOK_GELU, y=y, z=z))
+    assert torch.equal(mx.act_fwd(y)[0], z)
+
+
+def test_two_streams_at_once(mx):
+    """Calls on two streams that overlap on the GPU: each has its own buffers."""
+    y = [(torch.randn(4096, 1536, device="cuda") * 3).to(BF16) for _ in range(2)]
+    want = [mx.act_fwd(t) for t in y]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = [None, None]
+    for _ in range(5):
+        for k in range(2):
+            with torch.cuda.stream(streams[k]):
+                z, c = mx.act_fwd(y[k])
+                got[k] = (z, c, mx.act_bwd(z, c))
+    torch.cuda.synchronize()
+    for k in range(2):
+        assert torch.equal(got[k][0], want[k][0]) and torch.equal(got[k][1].codes, want[k][1].codes)
+        assert torch.equal(got[k][2], mx.act_bwd(want[k][0], want[k][1]))
+
+
 def test_act_over_its_input(mx):
     y = (torch.randn(65, 352, device="cuda") * 3).to(BF16)
     z, c = mx.act_fwd(y)

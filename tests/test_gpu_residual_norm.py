@@ -396,6 +396,25 @@ def test_captured_and_on_another_stream(mx):
         assert torch.equal(h, h2) and all(torch.equal(a, b) for a, b in zip(g, g2))
 
 
+def test_two_streams_at_once(mx):
+    cases = [Case(mx, 3000, 384, "layer", "rms", 3, seed=k) for k in range(2)]
+    want = []
+    for k in cases:
+        _, h, ctx = k.fwd()
+        want.append((h, mx.residual_norm_bwd(k.dh, k.dx_out, ctx)))
+    streams = [torch.cuda.Stream() for _ in cases]
+    torch.cuda.synchronize()
+    got = [None, None]
+    for _ in range(4):
+        for i, k in enumerate(cases):
+            with torch.cuda.stream(streams[i]):
+                _, h, ctx = k.fwd()
+                got[i] = (h, mx.residual_norm_bwd(k.dh, k.dx_out, ctx))
+    torch.cuda.synchronize()
+    for (h, g), (h2, g2) in zip(want, got):
+        assert torch.equal(h, h2) and all(torch.equal(a, b) for a, b in zip(g, g2))
+
+
 def test_against_differences(mx):
     """x_out in FP32 is linear in x, the gate and N_post's parameters: differences of the forward pass itself against its backward pass."""
     k = Case(mx, 48, 96, None, "layer", 4, F32, a=0.5, s=2.0)
