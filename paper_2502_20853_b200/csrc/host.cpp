@@ -336,10 +336,17 @@ bool tensor(PyObject *t, int64_t device, int dims, Rows &r)
     r.given = true;
     return !PyErr_Occurred();
 }
-// A matrix argument of `like`'s shape (if that is given) and of a type (-1: any).
+// A matrix argument of `like`'s shape (if that is given) and of a type (-1: any).  An address in its place: the binding has just allocated
+// it, of that shape and type and without gaps.
 bool matrix(PyObject *t, int64_t device, const Rows *like, int dtype, Rows &r)
 {
     if (t == Py_None) return true;
+    if (like && dtype >= 0 && PyLong_Check(t)) {
+        r = *like;
+        r.p = reinterpret_cast<void *>((uintptr_t)PyLong_AsUnsignedLongLongMask(t));
+        r.ld = like->cols, r.dtype = dtype;
+        return !PyErr_Occurred();
+    }
     if (!tensor(t, device, 2, r)) return false;
     if (like && (r.rows != like->rows || r.cols != like->cols)) return refuse("a matrix of another shape is expected");
     return dtype < 0 || r.dtype == dtype || refuse("a matrix of another type is expected");
