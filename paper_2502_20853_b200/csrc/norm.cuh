@@ -10,7 +10,9 @@
 // cannot hide the memory's latency by themselves; a lane's share of the next rows travels into shared memory meanwhile (cp.async, mostly
 // into slots that only this lane reads: no barriers of the block).
 // FULL: the lanes' vectors are exactly a row.  Without the masks of a partly filled lane the loops over V are straight code (25216 x 384
-// forward: 343 warp instructions per 256 columns with them, 213 without).
+// forward: 343 warp instructions per 256 columns with them, 213 without).  Otherwise teams are such that only a lane's last vector may be
+// missing, and the others have no masks either (47039 x 960 backward: 130 us with masks for all, 98 so; 50432 x 1056 forward: 138, 130); 32 and
+// 64 columns, on 4 lanes, have them.
 #pragma once
 #include <algorithm>
 
@@ -22,6 +24,9 @@ namespace mx {
 
 constexpr int kNormMaxCols = 8192;
 constexpr int kFwdThreads = 256;
+// Three blocks per SM where 80 registers and 74 KB each are enough and there is more to compute than a norm of full rows (50432 x 768 between two
+// layer norms 82 us with two, 73 with three, 50432 x 1056 with one 130, 114; 50432 x 768 with one, which has four stages of two blocks, 69, 71).
+constexpr int fwd_blocks_per_sm(int v, int x_bytes, bool post, bool full) { return v == 3 && x_bytes == 2 && (post || !full) ? 3 : 2; }
 // Backward: as many warps as the registers allow for v vectors of a lane and `sums` sums over rows (8 v registers each).  A kernel that
 // spills is twice as slow (50432 x 768: 80 us with eight warps, 158 with twelve and 200 bytes of spills): the ring leaves no L1 for them.
 constexpr int bwd_threads(int v, int sums) { return v == 4 ? 256 : v == 2 ? (sums == 2 ? 256 : 192) : sums == 2 ? 192 : 128; }
@@ -76,7 +81,7 @@ template <int N> __device__ __forceinline__ void lds8f(uint32_t slot, f2 (&o)[4]
     const uint4 a = lds16(slot), b = lds16(slot + N * 16);
     o[0] = (f2)a.y << 32 | a.x, o[1] = (f2)a.w << 32 | a.z, o[2] = (f2)b.y << 32 | b.x, o[3] = (f2)b.w << 32 | b.z;
 }
-constexpr int kRingBytes = 226 * 1024, kHalfRingBytes = 112 * 1024, kMostStages = 4;     // of an SM's one block, of one of two
+constexpr int kRingBytes = 226 * 1024, kHalfRingBytes = 112 * 1024, kThirdRingBytes = 74 * 1024, kMostStages = 4;     // of an SM's one block, of one of two
 // Waits until at most `left` (0 to 3) of this lane's groups of copies are under way.
 __device__ __forceinline__ void async_wait_all_but(int left)
 {
@@ -99,25 +104,33 @@ __device__ __forceinline__ void plane_get(const float4 *plane, int nvec, int vec
 __device__ __forceinline__ void zero8(f2 (&o)[4]) { o[0] = o[1] = o[2] = o[3] = 0; }
 
 // ---- teams --------------------------------------------------------------------------------------
-// L: its lanes of one warp (32, or fewer where a warp holds several teams).  Lane l of a team's warp w holds the vectors
-// 32 V w + i L + l, i < V.
+// L: its lanes of one warp (32, or fewer where a warp holds several teams).  Lane l of a warp whose part of the row starts at vector a holds
+// a + i L + l, i < V, as far as they are in that part; the warps' parts differ by at most one group of 32 columns.
 template <int L> struct Team {
     int warps, lane;     // of the team; of the warp's part of it
     int id, first_vec;   // of the team in its block; of the lane
+    int part_vecs;       // vectors of the warp's part
     bool leader;
     float4 *slots;       // several warps: where they leave their sums, two sets that take turns
     int turn;
 
-    __device__ __forceinline__ Team(int team_warps, int v, float4 *smem) : warps(team_warps), lane(threadIdx.x & (L - 1)), turn(0)
+    __device__ __forceinline__ Team(int team_warps, int nvec, float4 *smem) : warps(team_warps), lane(threadIdx.x & (L - 1)), part_vecs(nvec), turn(0)
     {
         const int part = L < 32 ? threadIdx.x / L : threadIdx.x >> 5;     // of a team, in the block
         id = L < 32 ? part : part / team_warps;
-        const int w = L < 32 ? 0 : part - id * team_warps;
-        first_vec = w * 32 * v + lane;
+        first_vec = lane;
+        if (L == 32 && team_warps > 1) {
+            const int w = part - id * team_warps, groups = nvec >> 2, each = groups / team_warps, more = groups - each * team_warps;
+            first_vec += (w * each + min(w, more)) * 4;
+            part_vecs = (each + (w < more)) * 4;
+        }
         leader = first_vec == 0;
         slots = smem + id * 2 * team_warps;
     }
 };
+
+// Whether a lane of a team has its vector i whatever its place: if not, that goes by the number that it has.
+template <int V, bool FULL, int L> __device__ __forceinline__ bool always(int i) { return FULL || (L > 4 && i < V - 1); }
 
 // Rows of which a team of several in a warp has none left take part in its shuffles; `turns` is the same for all teams of a warp.
 // (A warp that is in no team has no rows.)
@@ -190,7 +203,8 @@ struct RowPlan {
 };
 // Of 3 or 4 vectors per lane, and the fewest lanes that hold a row then, whatever leaves the fewest of a block's vectors without work; of both
 // 4 (fewer shuffles).  Backward (sums > 0) 2, 3 where that fills the lanes, or 4 where a block of shorter lanes would be one team.
-inline RowPlan row_plan(int64_t rows, int64_t cols, int sums)
+// More than 4 lanes only if each has its first k - 1 vectors.
+constexpr RowPlan row_plan(int64_t cols, int sums)
 {
     RowPlan b = {};
     const int64_t nvec = cols / 8;
@@ -200,17 +214,34 @@ inline RowPlan row_plan(int64_t rows, int64_t cols, int sums)
         int lanes = sums && k == 4 ? 32 : 4;
         while (lanes * k < nvec) lanes += lanes < 32 ? lanes : 32;
         if (sums && k == 3 && lanes * k != nvec) continue;
+        if (lanes > 4 && (lanes <= 32 ? nvec <= (k - 1) * lanes : nvec / 4 / (lanes / 32) < 8 * (k - 1))) continue;
         const int teams = threads / lanes, used = (int)(teams * nvec * 1000 / (threads * k));     // in thousandths
         if (teams > 0 && (sums ? used > best : used >= best)) b.v = k, b.lanes = lanes, b.teams = teams, best = used;
     }
     b.full = (int64_t)b.v * b.lanes * 8 == cols;
-    // forward up to three times as many blocks as are resident, as long as a team keeps six rows: 50432 x 768 with one, two, three, five times
-    // 74, 68, 69, 75 us, 8192 x 4096 48, 45, 44, 48, 25216 x 384 (five rows with one) 20.3, 24.8, 25.2, 25.2.  Backward each block has sums to
-    // leave, and more of them do not pay: 50432 x 768 with one, two, three times 75, 84, 92
-    const int64_t teams = b.teams, resident = (int64_t)kSms * (sums ? bwd_blocks_per_sm(b.v) : 2), most = ceil_div(rows, teams);
-    const int64_t times = sums ? 1 : std::min<int64_t>(std::max<int64_t>(rows / (resident * teams * 6), 1), 3);
-    b.rows_per_team = ceil_div(rows, std::min(most, resident * times) * teams);
-    b.blocks = (int)ceil_div(ceil_div(rows, b.rows_per_team), teams);     // blocks that have rows
+    return b;
+}
+constexpr bool each_width_has_a_plan()
+{
+    for (int64_t cols = 32; cols <= kNormMaxCols; cols += 32)
+        for (int sums = 0; sums <= 4; sums += sums ? 1 : 2)
+            if (row_plan(cols, sums).teams == 0 || row_plan(cols, sums).v * row_plan(cols, sums).lanes * 8 < cols) return false;
+    return true;
+}
+static_assert(each_width_has_a_plan());
+// Deals the rows to as many blocks as are resident, or `times` as many as long as a team keeps six rows.
+inline void deal(RowPlan &b, int64_t rows, int blocks_per_sm, int64_t times)
+{
+    const int64_t resident = (int64_t)kSms * blocks_per_sm, most = ceil_div(rows, b.teams);
+    times = std::min<int64_t>(std::max<int64_t>(rows / (resident * b.teams * 6), 1), times);
+    b.rows_per_team = ceil_div(rows, std::min(most, resident * times) * b.teams);
+    b.blocks = (int)ceil_div(ceil_div(rows, b.rows_per_team), b.teams);     // blocks that have rows
+}
+// Backward each block has sums to leave, and more blocks than are resident do not pay: 50432 x 768 with one, two, three times as many 75, 84, 92 us.
+inline RowPlan bwd_plan(int64_t rows, int64_t cols, int sums)
+{
+    RowPlan b = row_plan(cols, sums);
+    deal(b, rows, bwd_blocks_per_sm(b.v), 1);
     return b;
 }
 inline int64_t part_floats(const RowPlan &b, int64_t cols) { return (int64_t)b.blocks * 4 * cols; }

@@ -154,7 +154,7 @@ size_t mxfp4_residual_norm_workspace_bytes(int64_t rows, int64_t cols, int64_t g
     if (rows <= 0 || cols <= 0 || cols > kNormMaxCols || gates < 0) return 0;
     int64_t most = 0;      // whichever gradients are asked for
     for (int sums = 2; sums <= 4; sums++) {
-        const RowPlan b = row_plan(rows, cols, sums);
+        const RowPlan b = bwd_plan(rows, cols, sums);
         most = std::max(most, part_floats(b, cols) + slot_floats(b, cols, gates));
     }
     return (size_t)most * 4;
@@ -194,7 +194,7 @@ mxfp4_status_t mxfp4_residual_norm_bwd(const mxfp4_residual_norm_t *n, const mxf
     if (!workspace) return MXFP4_INVALID_ARG;
     if (reinterpret_cast<uintptr_t>(workspace) & 255u) return MXFP4_MISALIGNED;
     const bool sb = b->db_pre, sa = post && (b->db_post || (b->dgate && n->post.bias));
-    const RowPlan plan = row_plan(rows, cols, 2 + sb + sa);
+    const RowPlan plan = bwd_plan(rows, cols, 2 + sb + sa);
     if (workspace_bytes < mxfp4_residual_norm_workspace_bytes(rows, cols, n->gates)) return MXFP4_WORKSPACE_TOO_SMALL;
     {
         // dx and df are written row by row while later rows are still to be read

@@ -70,14 +70,12 @@ __global__ void __launch_bounds__(bwd_threads(V, 2 + SB + SA), bwd_blocks_per_sm
     __shared__ uint2 s_gates[N / L < N / 32 ? N / 32 : N / L];     // each team's first and last gate
     extern __shared__ __align__(128) uint8_t s_ring[];
     pdl_launch_dependents();
-    Team<L> t(p.warps, V, s_sum);
+    Team<L> t(p.warps, p.nvec, s_sum);
     const int64_t team = (int64_t)blockIdx.x * p.teams + t.id;
     // rows first, first + step, ...: side by side (see the forward pass), with several gates a run of rows for each team
     const int64_t first = t.id < p.teams ? min(p.several ? team * p.rows_per_team : team, p.rows) : p.rows, end = p.several ? min(first + p.rows_per_team, p.rows) : p.rows;
     const int64_t step = p.several ? 1 : (int64_t)gridDim.x * p.teams;
-    constexpr bool EXACT = FULL && L == 32;      // each turn of each lane has a row and all of its vectors
-    const int have = FULL ? V : max(0, min(V, (p.nvec - t.first_vec + L - 1) / L));
-    const int lanes = p.nvec - t.first_vec + t.lane;     // vectors of the row from this part's first lane on
+    const int have = FULL ? V : max(0, min(V, (t.part_vecs - t.lane + L - 1) / L));
     const float inv = 1.0f / (float)p.cols;
     const uint32_t base = (uint32_t)__cvta_generic_to_shared(s_ring);
     const uint32_t at16 = threadIdx.x * 16, at8 = threadIdx.x * 8;
@@ -91,16 +89,16 @@ __global__ void __launch_bounds__(bwd_threads(V, 2 + SB + SA), bwd_blocks_per_sm
         if (row < end) {
 #pragma unroll
             for (int i = 0; i < V; i++) {
-                const int l = FULL ? L : lanes - i * L;
+                const int l = always<V, FULL, L>(i) ? L : t.part_vecs - i * L;
                 if (p.dxo) async_row8<XT, L>(stage + i * kSlots<XT> * N * 16, dxo_at + i * L * 8, l);
                 if (PRE) {
                     async_row8<__nv_bfloat16, L>(stage + Ring::kDh + i * N * 16, dh_at + i * L * 8, l);
                     if (!EIGHT) async_row8<XT, L>(stage + Ring::kXh + i * kSlots<XT> * N * 16, xo_at + i * L * 8, l);
-                    else if (FULL || i < have) async8(stage + Ring::kXh + at8 + i * N * 8, xc_at + i * L * 8);
+                    else if (always<V, FULL, L>(i) || i < have) async8(stage + Ring::kXh + at8 + i * N * 8, xc_at + i * L * 8);
                 }
                 if (NEED_F) {
                     if (!EIGHT) async_row8<__nv_bfloat16, L>(stage + Ring::kFh + i * N * 16, f_at + i * L * 8, l);
-                    else if (FULL || i < have) async8(stage + Ring::kFh + at8 + i * N * 8, fc_at + i * L * 8);
+                    else if (always<V, FULL, L>(i) || i < have) async8(stage + Ring::kFh + at8 + i * N * 8, fc_at + i * L * 8);
                 }
             }
             dxo_at += step * p.lddxo;
@@ -125,7 +123,7 @@ __global__ void __launch_bounds__(bwd_threads(V, 2 + SB + SA), bwd_blocks_per_sm
         if (EIGHT) {
 #pragma unroll
             for (int i = 0; i < V; i++)
-                if (FULL || i < have) {
+                if (always<V, FULL, L>(i) || i < have) {
                     if (PRE) xs[i] = xs_at[i * (L / 4)];
                     if (NEED_F) fs[i] = fs_at[i * (L / 4)];
                 }
@@ -191,7 +189,7 @@ __global__ void __launch_bounds__(bwd_threads(V, 2 + SB + SA), bwd_blocks_per_sm
         float *o = gate == first_gate ? p.heads + team * 2 * p.cols : p.slots + ((int64_t)blockIdx.x + gate) * 2 * p.cols;
 #pragma unroll
         for (int i = 0; i < V; i++)
-            if (FULL || i < have) {
+            if (always<V, FULL, L>(i) || i < have) {
                 const int c = (i * L + t.first_vec) * 8;
                 store8(o + c, B[i]);
                 store8(o + p.cols + c, A[i]);
@@ -205,7 +203,7 @@ __global__ void __launch_bounds__(bwd_threads(V, 2 + SB + SA), bwd_blocks_per_sm
     const int turns = L < 32 ? (int)p.rows_per_team : first < end ? (int)((end - first + step - 1) / step) : 0;
     for (int k = 0; k < turns; k++, dx += step * p.lddx, df += step * p.lddf) {
         const int64_t row = first + k * step;
-        const bool live = EXACT || row < end;
+        const bool live = L == 32 || row < end;
         const int n = live ? have : 0;
         if (sizeof(XT) == 4) warp_sync();      // the others have read what is overwritten
         fetch(row + (S - 1) * step, base + (slot == 0 ? S - 1 : slot - 1) * Ring::kStage);
@@ -231,7 +229,7 @@ __global__ void __launch_bounds__(bwd_threads(V, 2 + SB + SA), bwd_blocks_per_sm
 #pragma unroll
         for (int i = 0; i < V; i++) {
             if (PRE) {
-                if (FULL || i < n) {
+                if (always<V, FULL, L>(i) || i < n) {
                     ring_row8<__nv_bfloat16>(stage + Ring::kDh + i * N * 16, d[i]);
                     if (EIGHT) {
                         e4m3_to8(lds8(stage + Ring::kXh + at8 + i * N * 8), xsc[i], xh[i]);
@@ -246,7 +244,7 @@ __global__ void __launch_bounds__(bwd_threads(V, 2 + SB + SA), bwd_blocks_per_sm
                 }
             }
         }
-        if (FULL && !EXACT && PRE && !live) {       // what the ring holds for a row that is none: a lane of a team beside a longer one
+        if (L < 32 && PRE && !live) {       // what the ring holds for a row that is none: a lane of a team beside a longer one
 #pragma unroll
             for (int i = 0; i < V; i++) zero8(d[i]), zero8(xh[i]);
         }
@@ -278,7 +276,7 @@ __global__ void __launch_bounds__(bwd_threads(V, 2 + SB + SA), bwd_blocks_per_sm
         f2 e1[V], e2[V];
 #pragma unroll
         for (int i = 0; i < V; i++) {
-            const bool on = FULL ? live : i < n;
+            const bool on = always<V, FULL, L>(i) ? live : i < n;
             f2 x[4];
             if (on) ring_row8<XT>(stage + i * kSlots<XT> * N * 16, x);
             else zero8(x);
@@ -345,7 +343,7 @@ __global__ void __launch_bounds__(bwd_threads(V, 2 + SB + SA), bwd_blocks_per_sm
         if (p.df && live) {
 #pragma unroll
             for (int i = 0; i < V; i++)
-                if (FULL || i < n) store8(df + i * L * 8, d[i]);
+                if (always<V, FULL, L>(i) || i < n) store8(df + i * L * 8, d[i]);
         }
     }
 
@@ -375,7 +373,7 @@ __global__ void __launch_bounds__(bwd_threads(V, 2 + SB + SA), bwd_blocks_per_sm
         if (t.leader) s_gates[t.id] = make_uint2(first_gate, gate);
 #pragma unroll
         for (int i = 0; i < V; i++)
-            if ((FULL || i < have) && in_team) {
+            if ((always<V, FULL, L>(i) || i < have) && in_team) {
                 float *o = last + (int64_t)t.id * 2 * cols + (i * L + t.first_vec) * 8;
                 store8(o, B[i]);
                 store8(o + cols, A[i]);

@@ -44,8 +44,8 @@ mxfp4_status_t mxfp4_residual_norm_fwd(const mxfp4_residual_norm_t *n, const voi
         !rows_over_or_apart(sh, ldh, 2, sf, ldf, 2) || meet(so, sh))
         return MXFP4_INVALID_ARG;
     NormFwd p = {};
-    const RowPlan plan = row_plan(rows, cols, 0);
-    p.warps = plan.warps(), p.teams = plan.teams, p.rows_per_team = plan.rows_per_team;
+    const RowPlan plan = row_plan(cols, 0);
+    p.warps = plan.warps(), p.teams = plan.teams;
     p.x = x, p.f = static_cast<const __nv_bfloat16 *>(f_bf16), p.xo = x_out, p.h = static_cast<__nv_bfloat16 *>(h_bf16);
     p.ldx = ldx, p.ldf = ldf, p.ldxo = ldxo, p.ldh = ldh;
     p.pre = side_of(n->pre), p.post = side_of(n->post);

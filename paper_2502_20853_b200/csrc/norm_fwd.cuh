@@ -2,8 +2,9 @@
 //     x' = a x + s g (w1 f^ + b1),  h = w2 x^ + b2;  f^ and x^ normalized in registers, the mean first and then the deviation around it
 // One read of x and f, one write of x', h and the checkpoints; per row four reductions over its lanes.  Bytes are the bound: x + f alone runs
 // at the copy rate (50432 x 1024 in FP32 78.7 us, 6.56 TB/s), with a norm and its checkpoint at 0.94 of it (bf16, 75.6 us), with norms and
-// checkpoints on both sides at 0.94 (FP32, RMS, 118 us) or, with layer norms and biases, 0.74 (768 columns, 81 us: the reductions' latency
-// and the planes' reads).  25216 x 384 with a layer scale: 19.5 us of 14.9 (five rows for each team, a start and an end of 2 us each).
+// checkpoints on both sides at 0.94 (FP32, RMS, 118 us) or, with layer norms and biases, 0.84 (1024 columns, 94 us: the reductions' latency
+// and the planes' reads; 768 columns in three blocks per SM 73 us, 0.82).  25216 x 384 with a layer scale: 19.5 us of 14.9 (five rows for
+// each team, a start and an end of 2 us each).
 #pragma once
 #include "norm.cuh"
 
@@ -62,7 +63,7 @@ __device__ __forceinline__ void normalize(Team<L> &t, const NormSide &n, float c
 #pragma unroll
         for (int i = 0; i < V; i++)
 #pragma unroll
-            for (int j = 0; j < 4; j++) v[i][j] = FULL || i < have ? f2_add(v[i][j], m2) : 0ull;     // zeros behind the row's end stay zeros
+            for (int j = 0; j < 4; j++) v[i][j] = always<V, FULL, L>(i) || i < have ? f2_add(v[i][j], m2) : 0ull;     // zeros behind the row's end stay zeros
     }
     f2 acc[V];
 #pragma unroll
@@ -114,7 +115,7 @@ __device__ __forceinline__ bool row_ckpt(const CkptOut &o, const Team<L> &t, int
         uint8_t *codes = o.codes + at * 8, *scales = o.scales + (at >> 2);
 #pragma unroll
         for (int i = 0; i < V; i++)
-            if (FULL || i < n) {
+            if (always<V, FULL, L>(i) || i < n) {
                 *reinterpret_cast<uint2 *>(codes + i * L * 8) = c[i];
                 if ((t.lane & 3) == 0) scales[i * (L / 4)] = (uint8_t)byte[i];
             }
@@ -132,23 +133,21 @@ template <class XT, int V, bool HAS_F> struct FwdRing {
 // x' = a x + (f^ cw + cb) [g], h = x^ pw + pb; cw = s w1 and cb = s b1, with one gate s g w1 and s g b1: the block keeps them in shared
 // memory as far as there are any (in registers they would leave room for eight warps instead of sixteen).
 template <class XT, int L, int V, bool FULL, bool HAS_F, bool POST, bool PRE>
-__global__ void __launch_bounds__(kFwdThreads, 2) k_norm_fwd(const __grid_constant__ NormFwd p)
+__global__ void __launch_bounds__(kFwdThreads, fwd_blocks_per_sm(V, sizeof(XT), POST, FULL)) k_norm_fwd(const __grid_constant__ NormFwd p)
 {
     using Ring = FwdRing<XT, V, HAS_F>;
     constexpr int N = kFwdThreads;
     __shared__ float4 s_sum[2 * (N / 32)];
     extern __shared__ __align__(128) uint8_t s_ring[];
     pdl_launch_dependents();
-    Team<L> t(p.warps, V, s_sum);
+    Team<L> t(p.warps, p.nvec, s_sum);
     const int64_t team = (int64_t)blockIdx.x * p.teams + t.id;
     // rows first, first + step, ...: what is read at a time lies side by side (401408 x 96: 73 us, with a run of rows for each team 98); where
     // gates come by way of L1 the block has a run of rows, for its teams to share them
     const bool runs = HAS_F && p.several && !p.gate_in_ring;
     const int64_t run = runs ? (int64_t)blockIdx.x * p.teams * p.rows_per_team : 0, end = runs ? min(run + p.teams * p.rows_per_team, p.rows) : p.rows;
     const int64_t step = runs ? p.teams : (int64_t)gridDim.x * p.teams, first = t.id < p.teams ? (runs ? run + t.id : team) : p.rows;
-    constexpr bool EXACT = FULL && L == 32;      // each turn of each lane has a row and all of its vectors
-    const int have = FULL ? V : max(0, min(V, (p.nvec - t.first_vec + L - 1) / L));   // vectors of this lane
-    const int lanes = p.nvec - t.first_vec + t.lane;     // vectors of the row from this part's first lane on
+    const int have = FULL ? V : max(0, min(V, (t.part_vecs - t.lane + L - 1) / L));   // vectors of this lane
     const float inv = 1.0f / (float)p.cols;
     const int S = p.stages, stage_bytes = Ring::kG + (p.gate_in_ring ? Ring::gate_bytes(p.gate_fp32) : 0);
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(s_ring);
@@ -162,11 +161,11 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_norm_fwd(const __grid_consta
         if (row < end) {
 #pragma unroll
             for (int i = 0; i < V; i++)
-                async_row8<XT, L>(stage + i * kSlots<XT> * N * 16, xp + i * L * 8, FULL ? L : lanes - i * L);
+                async_row8<XT, L>(stage + i * kSlots<XT> * N * 16, xp + i * L * 8, always<V, FULL, L>(i) ? L : t.part_vecs - i * L);
             if (HAS_F) {
 #pragma unroll
                 for (int i = 0; i < V; i++)
-                    async_row8<__nv_bfloat16, L>(stage + Ring::kF + i * N * 16, fp + i * L * 8, FULL ? L : lanes - i * L);
+                    async_row8<__nv_bfloat16, L>(stage + Ring::kF + i * N * 16, fp + i * L * 8, always<V, FULL, L>(i) ? L : t.part_vecs - i * L);
                 fp += step * p.ldf;
             }
             xp += step * p.ldx;
@@ -174,8 +173,8 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_norm_fwd(const __grid_consta
                 const int64_t g = (int64_t)((uint32_t)row / p.rows_per_gate) * p.ldg + t.first_vec * 8;
 #pragma unroll
                 for (int i = 0; i < V; i++) {
-                    if (p.gate_fp32) async_row8<float, L>(stage + Ring::kG + i * N * 32, static_cast<const float *>(p.gate) + g + i * L * 8, FULL ? L : lanes - i * L);
-                    else async_row8<__nv_bfloat16, L>(stage + Ring::kG + i * N * 16, static_cast<const __nv_bfloat16 *>(p.gate) + g + i * L * 8, FULL ? L : lanes - i * L);
+                    if (p.gate_fp32) async_row8<float, L>(stage + Ring::kG + i * N * 32, static_cast<const float *>(p.gate) + g + i * L * 8, always<V, FULL, L>(i) ? L : t.part_vecs - i * L);
+                    else async_row8<__nv_bfloat16, L>(stage + Ring::kG + i * N * 16, static_cast<const __nv_bfloat16 *>(p.gate) + g + i * L * 8, always<V, FULL, L>(i) ? L : t.part_vecs - i * L);
                 }
             }
         }
@@ -217,7 +216,7 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_norm_fwd(const __grid_consta
     const int turns = turns_of<L>(end, first, step);
     for (int k = 0; k < turns; k++) {
         const int64_t row = first + k * step;
-        const bool live = EXACT || row < end;
+        const bool live = L == 32 || row < end;
         if (sizeof(XT) == 4 || (HAS_F && p.gate_in_ring)) warp_sync();      // the others have read what is overwritten
         fetch(row + (S - 1) * step, ring + (slot == 0 ? S - 1 : slot - 1) * stage_bytes);
         const uint32_t stage = ring + slot * stage_bytes;
@@ -230,7 +229,7 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_norm_fwd(const __grid_consta
         if (HAS_F) {
 #pragma unroll
             for (int i = 0; i < V; i++) {
-                if (FULL || i < n) ring_row8<__nv_bfloat16>(stage + Ring::kF + i * N * 16, v[i]);
+                if (always<V, FULL, L>(i) || i < n) ring_row8<__nv_bfloat16>(stage + Ring::kF + i * N * 16, v[i]);
                 else zero8(v[i]);
             }
             if (POST) {
@@ -243,7 +242,7 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_norm_fwd(const __grid_consta
 #pragma unroll
                 for (int i = 0; i < V; i++) {
                     f2 w[4];
-                    if (FULL || i < have) plane_get(plane_cw, p.nvec, i * L + t.first_vec, w);
+                    if (always<V, FULL, L>(i) || i < have) plane_get(plane_cw, p.nvec, i * L + t.first_vec, w);
                     else zero8(w);
 #pragma unroll
                     for (int j = 0; j < 4; j++) v[i][j] = f2_mul(v[i][j], w[j]);
@@ -252,7 +251,7 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_norm_fwd(const __grid_consta
 #pragma unroll
                     for (int i = 0; i < V; i++) {
                         f2 w[4];
-                        if (FULL || i < have) plane_get(plane_cb, p.nvec, i * L + t.first_vec, w);
+                        if (always<V, FULL, L>(i) || i < have) plane_get(plane_cb, p.nvec, i * L + t.first_vec, w);
                         else zero8(w);
 #pragma unroll
                         for (int j = 0; j < 4; j++) v[i][j] = f2_fma(v[i][j], f2_of(r, r), w[j]);
@@ -264,7 +263,7 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_norm_fwd(const __grid_consta
 #pragma unroll
                     for (int i = 0; i < V; i++) {
                         f2 g[4];
-                        if (!(EXACT || i < n)) zero8(g);
+                        if (!((L == 32 && always<V, FULL, L>(i)) || i < n)) zero8(g);
                         else if (!p.gate_in_ring) load_param8(p.gate, p.gate_fp32, gate + i * L * 8, g);
                         else if (p.gate_fp32) ring_row8<float>(stage + Ring::kG + i * N * 32, g);
                         else ring_row8<__nv_bfloat16>(stage + Ring::kG + i * N * 16, g);
@@ -279,7 +278,7 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_norm_fwd(const __grid_consta
 #pragma unroll
             for (int i = 0; i < V; i++) {
                 f2 xx[4];
-                if (FULL || i < n) ring_row8<XT>(stage + i * kSlots<XT> * N * 16, xx);
+                if (always<V, FULL, L>(i) || i < n) ring_row8<XT>(stage + i * kSlots<XT> * N * 16, xx);
                 else zero8(xx);
                 if (p.a != 1.0f) {
 #pragma unroll
@@ -291,12 +290,12 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_norm_fwd(const __grid_consta
             if (p.xo && live) {
 #pragma unroll
                 for (int i = 0; i < V; i++)
-                    if (FULL || i < n) store8(xo + i * L * 8, v[i], p.wide);
+                    if (always<V, FULL, L>(i) || i < n) store8(xo + i * L * 8, v[i], p.wide);
             }
         } else {
 #pragma unroll
             for (int i = 0; i < V; i++) {
-                if (FULL || i < n) ring_row8<XT>(stage + i * kSlots<XT> * N * 16, v[i]);
+                if (always<V, FULL, L>(i) || i < n) ring_row8<XT>(stage + i * kSlots<XT> * N * 16, v[i]);
                 else zero8(v[i]);
             }
         }
@@ -309,7 +308,7 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_norm_fwd(const __grid_consta
 #pragma unroll
                 for (int i = 0; i < V; i++) {
                     f2 w[4];
-                    if (FULL || i < have) plane_get(plane_pw, p.nvec, i * L + t.first_vec, w);
+                    if (always<V, FULL, L>(i) || i < have) plane_get(plane_pw, p.nvec, i * L + t.first_vec, w);
                     else zero8(w);
 #pragma unroll
                     for (int j = 0; j < 4; j++) v[i][j] = f2_mul(v[i][j], w[j]);
@@ -319,7 +318,7 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_norm_fwd(const __grid_consta
 #pragma unroll
                 for (int i = 0; i < V; i++) {
                     f2 w[4];
-                    if (FULL || i < have) plane_get(plane_pb, p.nvec, i * L + t.first_vec, w);
+                    if (always<V, FULL, L>(i) || i < have) plane_get(plane_pb, p.nvec, i * L + t.first_vec, w);
                     else zero8(w);
 #pragma unroll
                     for (int j = 0; j < 4; j++) v[i][j] = f2_fma(v[i][j], f2_of(r, r), w[j]);
@@ -336,7 +335,7 @@ __global__ void __launch_bounds__(kFwdThreads, 2) k_norm_fwd(const __grid_consta
             if (p.h && live) {
 #pragma unroll
                 for (int i = 0; i < V; i++)
-                    if (FULL || i < n) *reinterpret_cast<uint4 *>(h + i * L * 8) = q[i];
+                    if (always<V, FULL, L>(i) || i < n) *reinterpret_cast<uint4 *>(h + i * L * 8) = q[i];
             }
             if (p.hq) {      // Q1 of the bf16 result, as the row-wise quantizer makes it
 #pragma unroll
@@ -380,14 +379,23 @@ template <class XT> cudaError_t launch_norm_fwd(NormFwd &p, const RowPlan &plan,
                 const size_t planes = (size_t)(p.has_cw + p.has_cb + (R && p.pre.w) + (R && p.pre.b)) * p.cols * 4;
                 // two stages in half of an SM's shared memory, or as many as there is room for in all of it (one at least: 128 KB of planes
                 // and 48 KB).  The row's gate travels with them if that does not take the second block's place (50432 x 1024 in FP32: 144 us
-                // with it and one block per SM, 127 with two and the gate by way of L1)
+                // with it and one block per SM, 127 with two and the gate by way of L1; 50432 x 768 with 256 gates 91 with it and two blocks, 85 with three)
                 using Ring = FwdRing<XT, V, F>;
-                const auto fits = [&](size_t stage) { return planes + 2 * stage <= kHalfRingBytes; };
+                constexpr bool FULL = decltype(full)::value;
+                const auto fits = [&](size_t stage, size_t room) { return planes + 2 * stage <= room; };
                 const size_t gate = p.several ? Ring::gate_bytes(p.gate_fp32) : 0;
-                p.gate_in_ring = p.several && fits(Ring::kG + gate);
-                const size_t stage = Ring::kG + (p.gate_in_ring ? gate : 0), room = fits(stage) ? kHalfRingBytes : kRingBytes;
+                const bool three = fwd_blocks_per_sm(V, sizeof(XT), Q, FULL) == 3 && fits(Ring::kG, kThirdRingBytes);
+                p.gate_in_ring = p.several && fits(Ring::kG + gate, three ? kThirdRingBytes : kHalfRingBytes);
+                const size_t stage = Ring::kG + (p.gate_in_ring ? gate : 0);
+                const int per_sm = three ? 3 : fits(stage, kHalfRingBytes) ? 2 : 1;
+                const size_t room = per_sm == 3 ? kThirdRingBytes : per_sm == 2 ? kHalfRingBytes : kRingBytes;
                 p.stages = (int)std::min<size_t>((room - planes) / stage, kMostStages);
-                return launch_ring<k_norm_fwd<XT, L, V, decltype(full)::value, F, Q, R>, kFwdThreads>(plan.blocks, p.stages * stage + planes, st, p);
+                // 50432 x 768 with one, two, three, five times as many blocks as are resident 74, 68, 69, 75 us, 8192 x 4096 48, 45, 44, 48,
+                // 25216 x 384 (five rows with one) 20.3, 24.8, 25.2, 25.2
+                RowPlan b = plan;
+                deal(b, p.rows, per_sm, 3);
+                p.rows_per_team = b.rows_per_team;
+                return launch_ring<k_norm_fwd<XT, L, V, FULL, F, Q, R>, kFwdThreads>(b.blocks, p.stages * stage + planes, st, p);
             }
         });
     };
