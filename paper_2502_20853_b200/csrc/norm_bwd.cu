@@ -21,6 +21,7 @@ struct NormBwdFinish {
     int blocks, pre, use_f, has_post, sb, sa;
     int64_t rows, rows_per_gate, rows_per_block;
     int cols, slices;         // slices of 128 columns
+    int warp_gates;           // a gate's slice is one warp's
     float *dw_pre, *db_pre, *dw_post, *db_post, *dgate;
 };
 
@@ -45,7 +46,7 @@ __device__ __forceinline__ float4 gate_gradient(const NormBwdFinish &p, int c, c
 }
 
 // Adds up what the blocks and teams have left, in a fixed order.  Two kinds of blocks: the first cols / 8 take 8 columns each, 2 lanes of
-// 4 columns by 128 lanes of rows, for the sums over all rows; then, where there are several gates, one for each gate and 128 columns.
+// 4 columns by 128 lanes of rows, for the sums over all rows; then, where there are several gates, one (or a warp of one) for each gate and 128 columns.
 // 3 to 5 us with the launch, of which 1.5 pass before the other kernel's results are visible.
 __global__ void __launch_bounds__(256) k_norm_bwd_finish(const __grid_constant__ NormBwdFinish p)
 {
@@ -125,21 +126,34 @@ __global__ void __launch_bounds__(256) k_norm_bwd_finish(const __grid_constant__
         put(p.dw_post, mul4(v[2], g)), put(p.db_post, mul4(v[3], g));
         return;
     }
-    const int job = blockIdx.x - p.cols / 8;
-    const int64_t g = job / p.slices;
-    const int c = (job - (int)g * p.slices) * 128 + lane * 4;
+    const int64_t job = p.warp_gates ? (int64_t)(blockIdx.x - p.cols / 8) * 8 + warp : blockIdx.x - p.cols / 8, g = job / p.slices;
+    const int c = (int)(job - g * p.slices) * 128 + lane * 4;
+    const bool on = g < p.gates && c < p.cols;
     const int64_t t0 = g * p.rows_per_gate / p.rows_per_block, t1 = ((g + 1) * p.rows_per_gate - 1) / p.rows_per_block;     // blocks
+    const float *at = p.slots + (t0 + g) * 2 * (int64_t)p.cols + c;
     float4 B = all4(0), A = all4(0);
-    if (c < p.cols)
-        for (int64_t k = t0 + warp; k <= t1; k += 8) {
-            const float *at = p.slots + (k + g) * 2 * (int64_t)p.cols + c;
-            add4(B, load4(at)), add4(A, load4(at + p.cols));
-        }
-    s_g[warp][0][lane] = B, s_g[warp][1][lane] = A;
-    __syncthreads();
-    if (warp > 0 || c >= p.cols) return;
+    if (p.warp_gates) {
+        float4 part[2][4];
 #pragma unroll
-    for (int k = 1; k < 8; k++) add4(B, s_g[k][0][lane]), add4(A, s_g[k][1][lane]);
+        for (int k = 0; k < 4; k++) {
+            part[0][k] = on && t0 + k <= t1 ? load4(at + k * 2 * p.cols) : all4(0);
+            part[1][k] = on && p.sa && t0 + k <= t1 ? load4(at + k * 2 * p.cols + p.cols) : all4(0);
+        }
+#pragma unroll
+        for (int k = 0; k < 4; k++) add4(B, part[0][k]), add4(A, part[1][k]);
+        if (!on) return;
+    } else {
+        if (on)
+            for (int64_t k = warp; k <= t1 - t0; k += 8) {
+                add4(B, load4(at + k * 2 * p.cols));
+                if (p.sa) add4(A, load4(at + k * 2 * p.cols + p.cols));
+            }
+        s_g[warp][0][lane] = B, s_g[warp][1][lane] = A;
+        __syncthreads();
+        if (warp > 0 || !on) return;
+#pragma unroll
+        for (int k = 1; k < 8; k++) add4(B, s_g[k][0][lane]), add4(A, s_g[k][1][lane]);
+    }
     *reinterpret_cast<float4 *>(p.dgate + g * p.cols + c) = gate_gradient(p, c, B, A);
 }
 
@@ -230,7 +244,9 @@ mxfp4_status_t mxfp4_residual_norm_bwd(const mxfp4_residual_norm_t *n, const mxf
     e.rows = rows, e.rows_per_gate = p.rows_per_gate, e.rows_per_block = plan.rows_per_team * plan.teams, e.cols = (int)cols;
     e.slices = (int)ceil_div(cols, 128);
     e.dw_pre = b->dw_pre, e.db_pre = b->db_pre, e.dw_post = b->dw_post, e.db_post = b->db_post, e.dgate = b->dgate;
-    const int64_t blocks = cols / 8 + (e.several && b->dgate ? e.gates * e.slices : 0);
+    // a warp takes a gate that at most four blocks have rows of, and eight warps one of more (47039 x 1024 with 2767 gates 158 us with eight for each, 99 so)
+    e.warp_gates = e.rows_per_gate <= 3 * e.rows_per_block;
+    const int64_t jobs = e.several && b->dgate ? e.gates * e.slices : 0, blocks = cols / 8 + (e.warp_gates ? ceil_div(jobs, 8) : jobs);
     MX_CHECK_CUDA(launch_pdl(k_norm_bwd_finish, (unsigned)blocks, 1, 256, 0, st, e));
     return MXFP4_OK;
 }

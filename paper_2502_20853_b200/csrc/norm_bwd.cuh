@@ -192,7 +192,7 @@ __global__ void __launch_bounds__(bwd_threads(V, 2 + SB + SA), bwd_blocks_per_sm
             if (always<V, FULL, L>(i) || i < have) {
                 const int c = (i * L + t.first_vec) * 8;
                 store8(o + c, B[i]);
-                store8(o + p.cols + c, A[i]);
+                if (SA) store8(o + p.cols + c, A[i]);
                 zero8(B[i]), zero8(A[i]);
             }
     };
@@ -376,7 +376,7 @@ __global__ void __launch_bounds__(bwd_threads(V, 2 + SB + SA), bwd_blocks_per_sm
             if ((always<V, FULL, L>(i) || i < have) && in_team) {
                 float *o = last + (int64_t)t.id * 2 * cols + (i * L + t.first_vec) * 8;
                 store8(o, B[i]);
-                store8(o + cols, A[i]);
+                if (SA) store8(o + cols, A[i]);
             }
     }
     __syncthreads();
@@ -395,7 +395,7 @@ __global__ void __launch_bounds__(bwd_threads(V, 2 + SB + SA), bwd_blocks_per_sm
         // along the block's teams: what they have of one gate follows each other, a team's first gate, (gates that are its own,) its last
         const int64_t row0 = (int64_t)blockIdx.x * p.teams * p.rows_per_team;
         const int with_rows = (int)min((int64_t)p.teams, (p.rows - row0 + p.rows_per_team - 1) / p.rows_per_team);
-        for (int c = threadIdx.x * 4; c < 2 * cols; c += N * 4) {
+        for (int c = threadIdx.x * 4; c < (SA ? 2 : 1) * cols; c += N * 4) {
             float4 v = make_float4(0, 0, 0, 0);
             uint32_t now = s_gates[0].x;
             const auto add = [&](const float *at) {
