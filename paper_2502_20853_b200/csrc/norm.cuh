@@ -213,7 +213,6 @@ constexpr RowPlan row_plan(int64_t cols, int sums)
         const int threads = sums ? bwd_threads(k, sums) : kFwdThreads;
         int lanes = sums && k == 4 ? 32 : 4;
         while (lanes * k < nvec) lanes += lanes < 32 ? lanes : 32;
-        if (sums && k == 3 && lanes * k != nvec) continue;
         if (lanes > 4 && (lanes <= 32 ? nvec <= (k - 1) * lanes : nvec / 4 / (lanes / 32) < 8 * (k - 1))) continue;
         const int teams = threads / lanes, used = (int)(teams * nvec * 1000 / (threads * k));     // in thousandths
         if (teams > 0 && (sums ? used > best : used >= best)) b.v = k, b.lanes = lanes, b.teams = teams, best = used;

@@ -443,7 +443,7 @@ template <class XT, bool EIGHT> cudaError_t launch_norm_bwd(const NormBwd &p, co
     const std::integral_constant<int, 3> three;
     const std::integral_constant<int, 4> four;
     if (plan.v == 2) return with_lanes<2>(plan, [&](auto l, auto full) { return go(l, two, full); });
-    if (plan.v == 3) return with_lanes<3>(plan, [&](auto l, auto) { return go(l, three, std::true_type()); });
+    if (plan.v == 3) return with_lanes<3>(plan, [&](auto l, auto full) { return go(l, three, full); });
     return plan.full ? go(L32(), four, std::true_type()) : go(L32(), four, std::false_type());
 }
 
