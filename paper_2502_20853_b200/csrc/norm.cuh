@@ -202,7 +202,10 @@ struct RowPlan {
     int warps() const { return lanes <= 32 ? 1 : lanes / 32; }
 };
 // Of 3 or 4 vectors per lane, and the fewest lanes that hold a row then, whatever leaves the fewest of a block's vectors without work; of both
-// 4 (fewer shuffles).  Backward (sums > 0) 2, 3 where that fills the lanes, or 4 where a block of shorter lanes would be one team.
+// 4 (fewer shuffles).  Backward (sums > 0) of 2, 3 or 4, of two alike 2 (43904 x 1024 with an RMS norm 68 us with 2, 70 with 4), or 3 if a block
+// has several teams (35136 x 1280 between layer norms 133 with 2, 116 with 3; 17536 x 2560, one team, 118 with 2, 125 with 3), and of all four
+// sums 4 (between layer norms 43904 x 1024 94 with 2, 84 with 4, 56192 x 800 135, 105; in FP32 from the inputs 141, 133 and 127, 152; if fewer
+// of its vectors have work it is not: 29248 x 1536 96, 118).
 // More than 4 lanes only if each has its first k - 1 vectors.
 constexpr RowPlan row_plan(int64_t cols, int sums)
 {
@@ -215,7 +218,8 @@ constexpr RowPlan row_plan(int64_t cols, int sums)
         while (lanes * k < nvec) lanes += lanes < 32 ? lanes : 32;
         if (lanes > 4 && (lanes <= 32 ? nvec <= (k - 1) * lanes : nvec / 4 / (lanes / 32) < 8 * (k - 1))) continue;
         const int teams = threads / lanes, used = (int)(teams * nvec * 1000 / (threads * k));     // in thousandths
-        if (teams > 0 && (sums ? used > best : used >= best)) b.v = k, b.lanes = lanes, b.teams = teams, best = used;
+        const bool of_two = !sums || (k == 3 && teams > 1) || (k == 4 && sums == 4);
+        if (teams > 0 && (used > best || (used == best && of_two))) b.v = k, b.lanes = lanes, b.teams = teams, best = used;
     }
     b.full = (int64_t)b.v * b.lanes * 8 == cols;
     return b;

@@ -45,10 +45,14 @@ template <class XT, int V, int SUMS, bool EIGHT, bool NEED_F, bool PRE> struct B
     static constexpr int kStage = kFh + (NEED_F ? (EIGHT ? 8 : 16) * kRow : 0);
     // behind the ring, also a lane's own: N_pre's weights, and s g w1 of the present gate, in FP32
     static constexpr int kW = PRE ? 32 * kRow : 0, kG = NEED_F ? 32 * kRow : 0;
-    static constexpr int kRoom = (bwd_blocks_per_sm(V) == 2 ? kHalfRingBytes : kRingBytes) - kW - kG;
+    // and the fourth sum of four vectors, which the registers have no room for (21952 x 2048 between layer norms 175 us with 184 bytes of
+    // spills, 93 so; 10944 x 4096 188, 104)
+    static constexpr bool kKeepA = V < 4 || SUMS < 4;
+    static constexpr int kA = kKeepA ? 0 : 32 * kRow;
+    static constexpr int kRoom = (bwd_blocks_per_sm(V) == 2 ? kHalfRingBytes : kRingBytes) - kW - kG - kA;
     static constexpr int kDepth = kRoom / kStage < kMostStages ? kRoom / kStage : kMostStages;
     static constexpr int kSums = 6 * 4 * 8 * kRow;       // at the end: up to six sums per column for each warp (team)
-    static constexpr int kBytes = kDepth * kStage + kW + kG > kSums ? kDepth * kStage + kW + kG : kSums;
+    static constexpr int kBytes = kDepth * kStage + kW + kG + kA > kSums ? kDepth * kStage + kW + kG + kA : kSums;
 };
 template <int N> __device__ __forceinline__ void sts8(uint32_t slot, const f2 (&v)[4])
 {
@@ -166,7 +170,7 @@ __global__ void __launch_bounds__(bwd_threads(V, 2 + SB + SA), bwd_blocks_per_sm
 #pragma unroll
     for (int k = 0; k < S - 1; k++) fetch(first + k * step, base + k * Ring::kStage);
 
-    const uint32_t w_at = base + S * Ring::kStage + at16, g_at = w_at + Ring::kW;
+    const uint32_t w_at = base + S * Ring::kStage + at16, g_at = w_at + Ring::kW, a_at = g_at + Ring::kG;
     if (PRE) {
 #pragma unroll
         for (int i = 0; i < V; i++) sts8<N>(w_at + i * N * 32, w1[i]);
@@ -183,6 +187,10 @@ __global__ void __launch_bounds__(bwd_threads(V, 2 + SB + SA), bwd_blocks_per_sm
     f2 sw[V][4], sb[V][4], B[V][4], A[V][4];
 #pragma unroll
     for (int i = 0; i < V; i++) zero8(sw[i]), zero8(sb[i]), zero8(B[i]), zero8(A[i]);
+    const auto get_A = [&](int i) { if (!Ring::kKeepA) lds8f<N>(a_at + i * N * 32, A[i]); };
+    const auto put_A = [&](int i) { if (!Ring::kKeepA) sts8<N>(a_at + i * N * 32, A[i]); };
+#pragma unroll
+    for (int i = 0; i < V; i++) put_A(i);
     if (NEED_F) put_gate();
     const uint32_t first_gate = gate;
     const auto flush = [&]() {     // the rows of a gate are done and the team goes on: its first one is left to the block's end, any other is whole
@@ -192,8 +200,10 @@ __global__ void __launch_bounds__(bwd_threads(V, 2 + SB + SA), bwd_blocks_per_sm
             if (always<V, FULL, L>(i) || i < have) {
                 const int c = (i * L + t.first_vec) * 8;
                 store8(o + c, B[i]);
+                get_A(i);
                 if (SA) store8(o + p.cols + c, A[i]);
                 zero8(B[i]), zero8(A[i]);
+                put_A(i);
             }
     };
 
@@ -311,6 +321,7 @@ __global__ void __launch_bounds__(bwd_threads(V, 2 + SB + SA), bwd_blocks_per_sm
                 }
                 f2 w[4];
                 lds8f<N>(g_at + i * N * 32, w);
+                get_A(i);
 #pragma unroll
                 for (int j = 0; j < 4; j++) {
                     B[i][j] = f2_fma(x[j], xh[i][j], B[i][j]);
@@ -321,6 +332,7 @@ __global__ void __launch_bounds__(bwd_threads(V, 2 + SB + SA), bwd_blocks_per_sm
                         e2[i] = j ? f2_fma(d[i][j], xh[i][j], e2[i]) : f2_mul(d[i][j], xh[i][j]);
                     }
                 }
+                put_A(i);
             } else {
 #pragma unroll
                 for (int j = 0; j < 4; j++) d[i][j] = f2_mul(x[j], f2_of(p.s, p.s));
@@ -349,6 +361,8 @@ __global__ void __launch_bounds__(bwd_threads(V, 2 + SB + SA), bwd_blocks_per_sm
 
     // the block's sums: teams of one warp by shuffles, then each warp's (team's) sums side by side in shared memory
     async_wait<0>();
+#pragma unroll
+    for (int i = 0; i < V; i++) get_A(i);
     __syncthreads();
     const int wide = p.warps * 32, parts = L < 32 ? N / 32 : p.teams, cols = p.cols;
     const bool in_team = L < 32 || t.id < p.teams;
