@@ -325,6 +325,21 @@ def test_many_rows(mx, cols, rows, gates):
         torch.cuda.empty_cache()
 
 
+# widths whose rows do not fill their lanes: the parts of a row's warps differ by a group, a lane's last vector is missing; with the sums of one
+# norm without biases (2), with them, and of two norms with them (4)
+@pytest.mark.parametrize("cols", [320, 416, 480, 544, 640, 992, 1120, 1152, 1280, 1312, 1440, 1824, 2272, 2560, 2592, 3104, 4160, 5120, 5472, 6048, 6336, 7328])
+@pytest.mark.parametrize("post,bias", [(None, False), (None, True), ("layer", True)])
+def test_rows_that_do_not_fill_their_lanes(mx, cols, post, bias):
+    for dtype, save in ((BF16, mx.SAVE_8BIT), (F32, mx.SAVE_INPUTS), (F32, mx.SAVE_8BIT)):
+        _both_ways(Case(mx, 41, cols, "layer", post, 1, dtype, bias=bias, seed=cols), save)
+
+
+@pytest.mark.parametrize("rows,cols,gates", [(9000, 160, 9000), (12000, 640, 800), (12000, 1056, 40), (9000, 1024, 3), (6000, 2080, 1500), (1212, 4128, 606), (700, 8192, 7)])
+@pytest.mark.parametrize("bias", [False, True])
+def test_gates_of_few_and_of_many_blocks(mx, rows, cols, gates, bias):
+    _both_ways(Case(mx, rows, cols, "rms", "layer", gates, BF16, bias=bias), mx.SAVE_8BIT)
+
+
 def test_kept_inputs_are_not_written_over(mx):
     k = Case(mx, 8, 96, "layer", "rms", 1)
     with pytest.raises(AssertionError):
