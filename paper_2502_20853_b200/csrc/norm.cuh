@@ -4,7 +4,7 @@
 // through shuffles and, where a team has several warps, through shared memory and a barrier of the team.  V (2 to 4
 // backward, 3 or 4 forward) and the lanes are chosen so that a block's lanes have the most to do (row_plan); the usual widths are reached
 // exactly.
-// Two blocks per SM, and for long matrices several times as many blocks as fit: the SMs do not get equal shares of the memory's bandwidth (in
+// Two or three blocks per SM, and for long matrices forward several times as many blocks as fit: the SMs do not get equal shares of the memory's bandwidth (in
 // a kernel of one block per SM the mean SM was done at 81 % of the last one's time), so what is left is dealt out as they finish.  A block's
 // lanes keep their columns from row to row: what belongs to a column (weights, a gate, sums over rows) is fetched once.  The few warps
 // cannot hide the memory's latency by themselves; a lane's share of the next rows travels into shared memory meanwhile (cp.async, mostly
