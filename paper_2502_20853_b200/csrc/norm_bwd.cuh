@@ -162,11 +162,13 @@ __global__ void __launch_bounds__(bwd_threads(V, 2 + SB + SA), bwd_blocks_per_sm
     }
     if (NEED_F) get_gate(first < end ? gate : 0);
     fetch_small(first);
-    if (!p.dxo) {       // nothing comes from further on: the slots stay zeros
+    if (!p.dxo) {       // nothing comes from further on: the slots stay zeros, each written by the lane that reads it (ring_row8), for no barrier follows
         for (int k = 0; k < S; k++)
 #pragma unroll
-            for (int i = 0; i < V * kSlots<XT>; i++)
-                asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(base + k * Ring::kStage + at16 + i * N * 16), "r"(0) : "memory");
+            for (int i = 0; i < V; i++)
+#pragma unroll
+                for (int j = 0; j < kSlots<XT>; j++)
+                    asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(base + k * Ring::kStage + at16 * kSlots<XT> + (i * kSlots<XT> * N + j) * 16), "r"(0) : "memory");
     }
 #pragma unroll
     for (int k = 0; k < S - 1; k++) fetch(first + k * step, base + k * Ring::kStage);
