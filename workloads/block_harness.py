@@ -78,10 +78,11 @@ class _MxLinearFn(torch.autograd.Function):
 
 
 class _NormFn(torch.autograd.Function):
-    """x + f (f may be None) and, where ``norm`` is given, its norm; the call's tensors go into ``record``."""
+    """x + f (f may be None) and, where ``weight`` and ``bias`` are given, its layer norm; the call's tensors go into ``record``."""
 
     @staticmethod
-    def forward(ctx, x, f, mx, norm, hq, record, status):
+    def forward(ctx, x, f, weight, bias, eps, mx, hq, record, status):
+        norm = mx.Norm(mx.NORM_LAYER, weight.detach(), bias.detach(), eps) if weight is not None else None
         x2, f2 = x.reshape(-1, D_MODEL), f.reshape(-1, D_MODEL) if f is not None else None
         x_out, h, nctx = mx.residual_norm_fwd(x2, f2, pre=norm, hq=hq, dev_status=status)
         ctx.mx, ctx.nctx, ctx.record, ctx.shape = mx, nctx, record, x.shape
@@ -93,7 +94,9 @@ class _NormFn(torch.autograd.Function):
         d = lambda t: t.reshape(-1, D_MODEL).contiguous() if t is not None else None  # noqa: E731
         g = ctx.mx.residual_norm_bwd(d(dh), d(dx_out), ctx.nctx, df=None if ctx.record["f"] is not None else False)
         ctx.record.update(dh=d(dh), dx_out=d(dx_out), grads=g)
-        return g.dx.reshape(ctx.shape), g.df.reshape(ctx.shape) if g.df is not None else None, None, None, None, None, None
+        norm = ctx.nctx.pre
+        dw, db = (g.pre_weight.to(norm.weight.dtype), g.pre_bias.to(norm.bias.dtype)) if norm is not None else (None, None)
+        return g.dx.reshape(ctx.shape), g.df.reshape(ctx.shape) if g.df is not None else None, dw, db, None, None, None, None, None
 
 
 class _GeluFn(torch.autograd.Function):
@@ -140,10 +143,10 @@ class Block:
     def _norm(self, name, x, f, ln):
         """(x + f, its norm, Q1 of that)"""
         mx, rows = self.mx, x.numel() // D_MODEL
-        norm = mx.Norm(mx.NORM_LAYER, ln.weight.detach(), ln.bias.detach(), ln.eps) if ln is not None else None
+        weight, bias, eps = (ln.weight, ln.bias, ln.eps) if ln is not None else (None, None, None)
         hq = mx.QMat(rows, D_MODEL) if ln is not None else None
         self.records[name] = {}
-        return (*_NormFn.apply(x, f, mx, norm, hq, self.records[name], self.status), hq)
+        return (*_NormFn.apply(x, f, weight, bias, eps, mx, hq, self.records[name], self.status), hq)
 
     def _forward_fused(self, x):
         B, T, D = x.shape
