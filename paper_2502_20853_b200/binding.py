@@ -874,8 +874,9 @@ def residual_norm_fwd(x, f=None, pre=None, post=None, gate=None, residual_scale=
                 f_at = kf._at(shape, dev)
         else:
             kx, kf = (x_out if f is not None else x) if pre is not None else None, f if keep_f else None
-            assert h is None or all(t is None or h.data_ptr() != t.data_ptr() for t in (kx, kf)), "what is kept must not be written over"
-            assert kf is None or x_out is None or x_out.data_ptr() != kf.data_ptr(), "what is kept must not be written over"
+            if rows:        # (tensors without elements all have the address 0)
+                assert h is None or all(t is None or h.data_ptr() != t.data_ptr() for t in (kx, kf)), "what is kept must not be written over"
+                assert kf is None or x_out is None or x_out.data_ptr() != kf.data_ptr(), "what is kept must not be written over"
         ctx = NormCtx(kx, kf, stats, pre, post, gate, residual_scale, branch_scale)
     _check("mxfp4_residual_norm_fwd", _host.residual_norm_fwd(lib().at_residual_norm_fwd, dev, x, f, pre, post, gate, residual_scale, branch_scale, x_to, h_to, hq,
                                                               _ptr(stats), *x_at, *f_at, scale_mode, _ptr(dev_status), _stream()))
