@@ -845,7 +845,10 @@ def residual_norm_fwd(x, f=None, pre=None, post=None, gate=None, residual_scale=
     are), or nothing.  Returns (x_out, h, NormCtx or None)."""
     shape = rows, cols = x.shape
     where = x.device
-    x_to, h_to = x_out, h       # as the native module takes them: what is allocated here by its address
+    # as the native module takes them: what is allocated here by its address, which nothing from outside may pass for
+    x_to, h_to = x_out, h
+    assert x_out is None or isinstance(x_out, torch.Tensor), "x_out: a tensor"
+    assert h is None or h is False or isinstance(h, torch.Tensor), "h: a tensor, or False for none"
     if f is None:
         assert x_out is None
     elif x_out is None:
@@ -905,6 +908,7 @@ def residual_norm_bwd(dh, dx_out, ctx, dx=None, df=None, workspace=None):
     elif df is False:
         df = None
     else:
+        assert isinstance(df, torch.Tensor), "df: a tensor, or False for none"
         df_to = df
     x_at = f_at = (None, None)
     if isinstance(x, Checkpoint):

@@ -336,20 +336,23 @@ bool tensor(PyObject *t, int64_t device, int dims, Rows &r)
     r.given = true;
     return !PyErr_Occurred();
 }
-// A matrix argument of `like`'s shape (if that is given) and of a type (-1: any).  An address in its place: the binding has just allocated
-// it, of that shape and type and without gaps.
+// A matrix argument of `like`'s shape (if that is given) and of a type (-1: any).
 bool matrix(PyObject *t, int64_t device, const Rows *like, int dtype, Rows &r)
 {
     if (t == Py_None) return true;
-    if (like && dtype >= 0 && PyLong_Check(t)) {
-        r = *like;
-        r.p = reinterpret_cast<void *>((uintptr_t)PyLong_AsUnsignedLongLongMask(t));
-        r.ld = like->cols, r.dtype = dtype;
-        return !PyErr_Occurred();
-    }
     if (!tensor(t, device, 2, r)) return false;
     if (like && (r.rows != like->rows || r.cols != like->cols)) return refuse("a matrix of another shape is expected");
     return dtype < 0 || r.dtype == dtype || refuse("a matrix of another type is expected");
+}
+// One of the outputs that the binding allocates itself unless its caller gives them (a tensor, which the binding has looked at): then their
+// address comes in their place, of `like`'s shape and without gaps.
+bool output(PyObject *t, int64_t device, const Rows &like, int dtype, Rows &r)
+{
+    if (!PyLong_Check(t)) return matrix(t, device, &like, dtype, r);
+    r = like;
+    r.p = reinterpret_cast<void *>((uintptr_t)PyLong_AsUnsignedLongLongMask(t));
+    r.ld = like.cols, r.dtype = dtype;
+    return !PyErr_Occurred();
 }
 bool norm_of(PyObject *o, int64_t device, int64_t cols, mxfp4_norm_t &n)
 {
@@ -411,7 +414,7 @@ PyObject *h_norm_fwd(PyObject *, PyObject *const *a, Py_ssize_t n)
     mxfp4_residual_norm_t plan;
     if (a[2] == Py_None) refuse("x is expected");
     if (a[2] == Py_None || !matrix(a[2], device, nullptr, -1, x) || !matrix(a[3], device, &x, MXFP4_OUT_BF16, b) || !plan_of(a + 4, device, x, x.dtype, plan) ||
-        !matrix(a[9], device, &x, x.dtype, xo) || !matrix(a[10], device, &x, MXFP4_OUT_BF16, h))
+        !output(a[9], device, x, x.dtype, xo) || !output(a[10], device, x, MXFP4_OUT_BF16, h))
         return nullptr;
     const mxfp4_mat_t hq = r.dst(11);
     const bool with_hq = r.given(11);
@@ -436,7 +439,7 @@ PyObject *h_norm_bwd(PyObject *, PyObject *const *a, Py_ssize_t n)
     if (a[16] == Py_None) refuse("dx is expected");
     if (a[16] == Py_None || !matrix(a[16], device, nullptr, -1, dx) || !matrix(a[2], device, &dx, MXFP4_OUT_BF16, dh) || !matrix(a[3], device, &dx, dx.dtype, dxo) ||
         !plan_of(a + 4, device, dx, dx.dtype, plan) || !matrix(a[9], device, nullptr, MXFP4_OUT_FP32, st) || !matrix(a[10], device, &dx, dx.dtype, x) ||
-        !matrix(a[11], device, &dx, MXFP4_OUT_BF16, b) || !matrix(a[17], device, &dx, MXFP4_OUT_BF16, df))
+        !matrix(a[11], device, &dx, MXFP4_OUT_BF16, b) || !output(a[17], device, dx, MXFP4_OUT_BF16, df))
         return nullptr;
     if (st.given && (st.rows != 4 || st.cols != dx.rows || (st.ld != st.cols && st.cols > 0))) {
         refuse("the statistics are [4, rows], without gaps");

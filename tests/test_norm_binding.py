@@ -24,3 +24,27 @@ def test_no_rows(save, with_f):
     norm = mx.Norm(mx.NORM_LAYER, torch.ones(96), torch.zeros(96))
     x_out, h, ctx = mx.residual_norm_fwd(x, f if with_f else None, pre=norm, post=norm if with_f else None, gate=torch.ones(96) if with_f else None, save=save)
     assert h.shape == (0, 96) and (x_out is None) == (not with_f) and (ctx is None) == (save == mx.SAVE_NOTHING)
+
+
+def _plan(rows=4):
+    x, f = torch.zeros(rows, 96), torch.zeros(rows, 96, dtype=BF16)
+    norm = mx.Norm(mx.NORM_LAYER, torch.ones(96), torch.zeros(96))
+    return x, f, norm
+
+
+@pytest.mark.parametrize("number", [0, 1, True, 1 << 40])
+def test_numbers_are_not_addresses(number):
+    """A number in a matrix's place is refused, not written to."""
+    x, f, norm = _plan()
+    for kw in (dict(x_out=number), dict(h=number)):
+        with pytest.raises(AssertionError):
+            mx.residual_norm_fwd(x, f, pre=norm, **kw)
+    with pytest.raises((AssertionError, AttributeError, TypeError)):
+        mx.residual_norm_fwd(x, number, pre=norm)
+    ctx = mx.NormCtx(torch.zeros(4, 96), f, torch.zeros(4, 4), norm, norm)
+    for args, kw in (((f, x), dict(df=number)), ((f, x), dict(dx=number)), ((f, number), dict(dx=x)), ((number, x), dict(df=f))):
+        with pytest.raises((AssertionError, AttributeError, TypeError)):
+            mx.residual_norm_bwd(*args, ctx, workspace=torch.empty(1 << 20, dtype=torch.uint8), **kw)
+    for kept in ((number, f), (x, number)):
+        with pytest.raises((AssertionError, AttributeError, TypeError)):
+            mx.residual_norm_bwd(f, x, mx.NormCtx(*kept, torch.zeros(4, 4), norm, norm), workspace=torch.empty(1 << 20, dtype=torch.uint8))
