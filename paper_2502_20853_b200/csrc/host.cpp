@@ -395,6 +395,7 @@ bool plan_of(PyObject *const *a, int64_t device, const Rows &x, int32_t x_dtype,
         Py_DECREF(shape);
         if (!tensor(a[2], device, dims, g)) return false;
         if (g.cols != x.cols) return refuse("the gate has a number for each column");
+        if (g.rows == 0 && x.rows > 0) return refuse("a gate for each run of rows is expected");
         n.gate = g.p, n.gates = g.rows, n.ld_gate = g.ld, n.gate_dtype = g.dtype;
     }
     n.residual_scale = (float)PyFloat_AsDouble(a[3]);

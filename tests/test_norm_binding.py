@@ -48,3 +48,16 @@ def test_numbers_are_not_addresses(number):
     for kept in ((number, f), (x, number)):
         with pytest.raises((AssertionError, AttributeError, TypeError)):
             mx.residual_norm_bwd(f, x, mx.NormCtx(*kept, torch.zeros(4, 4), norm, norm), workspace=torch.empty(1 << 20, dtype=torch.uint8))
+
+
+def test_gate_without_rows():
+    """[0, cols] is no gate at all, not one of 1."""
+    x, f, norm = _plan()
+    gate = torch.empty(0, 96)
+    with pytest.raises(AssertionError, match="gate"):
+        mx.residual_norm_fwd(x, f, pre=norm, gate=gate)
+    ctx = mx.NormCtx(torch.zeros(4, 96), f, torch.zeros(4, 4), norm, norm, gate)
+    with pytest.raises(AssertionError, match="gate"):
+        mx.residual_norm_bwd(f, x, ctx, workspace=torch.empty(1 << 20, dtype=torch.uint8))
+    x_out, _, _ = mx.residual_norm_fwd(x[:0], f[:0], pre=norm, gate=gate)
+    assert x_out.shape == (0, 96)
