@@ -708,6 +708,12 @@ def change_sums(cur, prev, out=None):
 _DTYPES = (torch.bfloat16, torch.float32)     # by MXFP4_OUT_*
 
 
+def _status(t, dev):
+    """The address of a status word, which is on the device of the call."""
+    assert t is None or t.get_device() == dev, "a status word on the current device is expected"
+    return _ptr(t)
+
+
 class Checkpoint:
     """An activation kept in 8 bits: E4M3 ``codes`` (uint8 [rows, cols]) and one E8M0 byte per 32 columns, ``scales`` (uint8 [rows, cols / 32]).
     Those that the binding allocates itself share one buffer; ``codes`` and ``scales`` are views of it, made when they are asked for."""
@@ -767,7 +773,7 @@ def checkpoint_store(x, scale_mode=SCALE_TRUNCATION_FREE, out=None, dev_status=N
         out = Checkpoint.empty(rows, cols, x.device)
     dev = _device()
     _check("mxfp4_checkpoint_store",
-           _host.checkpoint_store(lib().at_checkpoint_store, dev, x, *out._at((rows, cols), dev), scale_mode, _ptr(dev_status), _stream()))
+           _host.checkpoint_store(lib().at_checkpoint_store, dev, x, *out._at((rows, cols), dev), scale_mode, _status(dev_status, dev), _stream()))
     return out
 
 
@@ -796,7 +802,7 @@ def act_fwd(y, act=ACT_GELU, save=SAVE_8BIT, scale_mode=SCALE_TRUNCATION_FREE, o
         ckpt = Checkpoint.empty(rows, cols, y.device)
     dev = _device()
     _check("mxfp4_act_fwd", _host.act_fwd(lib().at_act_fwd, dev, y, act, out, *(ckpt._at((rows, cols), dev) if ckpt is not None else (None, None)), scale_mode,
-                                          _ptr(dev_status), _stream()))
+                                          _status(dev_status, dev), _stream()))
     return out, ckpt
 
 
@@ -862,6 +868,7 @@ def residual_norm_fwd(x, f=None, pre=None, post=None, gate=None, residual_scale=
         h_to = h.data_ptr()
     dev = _device()
     kx = kf = stats = ctx = None
+    assert hq is None or hq.device == where, "a quantized matrix on x's device is expected"
     x_at = f_at = (None, None)
     if save != SAVE_NOTHING:
         assert save in (SAVE_8BIT, SAVE_INPUTS)
@@ -882,7 +889,7 @@ def residual_norm_fwd(x, f=None, pre=None, post=None, gate=None, residual_scale=
                 assert kf is None or x_out is None or x_out.data_ptr() != kf.data_ptr(), "what is kept must not be written over"
         ctx = NormCtx(kx, kf, stats, pre, post, gate, residual_scale, branch_scale)
     _check("mxfp4_residual_norm_fwd", _host.residual_norm_fwd(lib().at_residual_norm_fwd, dev, x, f, pre, post, gate, residual_scale, branch_scale, x_to, h_to, hq,
-                                                              _ptr(stats), *x_at, *f_at, scale_mode, _ptr(dev_status), _stream()))
+                                                              _ptr(stats), *x_at, *f_at, scale_mode, _status(dev_status, dev), _stream()))
     return x_out, h, ctx
 
 
@@ -923,6 +930,8 @@ def residual_norm_bwd(dh, dx_out, ctx, dx=None, df=None, workspace=None):
     gg = _new((gates, cols), torch.float32, where) if gates else None
     if workspace is None:
         workspace = _new((max(residual_norm_workspace_bytes(rows, cols, gates), 256),), torch.uint8, where)
+    else:
+        assert workspace.get_device() == dev and workspace.is_contiguous(), "a workspace on the current device, without gaps, is expected"
     _check("mxfp4_residual_norm_bwd",
            _host.residual_norm_bwd(lib().at_residual_norm_bwd, dev, dh, dx_out, pre, post, gate, ctx.residual_scale, ctx.branch_scale, ctx.stats, x, f, *x_at, *f_at,
                                    dx, df_to, _ptr(gw), _ptr(gb), _ptr(qw), _ptr(qb), _ptr(gg), workspace.data_ptr(), workspace.numel(), _stream()))

@@ -61,3 +61,33 @@ def test_gate_without_rows():
         mx.residual_norm_bwd(f, x, ctx, workspace=torch.empty(1 << 20, dtype=torch.uint8))
     x_out, _, _ = mx.residual_norm_fwd(x[:0], f[:0], pre=norm, gate=gate)
     assert x_out.shape == (0, 96)
+
+
+class _Elsewhere:
+    """A tensor that says that it is on another device than the call's."""
+
+    def __init__(self, t):
+        self.t, self.device = t, torch.device("cuda", 1)
+
+    def get_device(self):
+        return 1
+
+    def __getattr__(self, name):
+        return getattr(self.t, name)
+
+
+def test_what_comes_beside_the_matrices_is_on_their_device():
+    x, f, norm = _plan()
+    status, work = _Elsewhere(torch.zeros(1, dtype=torch.int32)), torch.empty(1 << 20, dtype=torch.uint8)
+    hq = mx.QMat(4, 96, "meta", torch.empty(4, 48, dtype=torch.uint8, device="meta"), torch.empty(512, dtype=torch.uint8, device="meta"))
+    for kw in (dict(dev_status=status), dict(hq=hq)):
+        with pytest.raises(AssertionError):
+            mx.residual_norm_fwd(x, f, pre=norm, **kw)
+    with pytest.raises(AssertionError):
+        mx.act_fwd(f, dev_status=status)
+    with pytest.raises(AssertionError):
+        mx.checkpoint_store(x, dev_status=status)
+    ctx = mx.NormCtx(torch.zeros(4, 96), f, torch.zeros(4, 4), norm, norm)
+    for w in (_Elsewhere(work), work[::2]):
+        with pytest.raises(AssertionError, match="workspace"):
+            mx.residual_norm_bwd(f, x, ctx, workspace=w)
