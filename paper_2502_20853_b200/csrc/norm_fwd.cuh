@@ -81,6 +81,8 @@ __device__ __forceinline__ void normalize(Team<L> &t, const NormSide &n, float c
     rstd = x > 0.0f && x < __uint_as_float(0x7F800000u) ? fmaf(0.5f * r, fmaf(-x * r, r, 1.0f), r) : r;
 }
 
+constexpr float kFinite = 3.40282347e38f;
+
 // The checkpoint of the row v r.  `n`: vectors of this lane that are written; `at`: where the lane's first one is, in eights of the matrix.
 template <int V, bool FULL, int L>
 __device__ __forceinline__ bool row_ckpt(const CkptOut &o, const Team<L> &t, int n, const f2 (&v)[V][4], float r, int64_t at)
@@ -95,14 +97,15 @@ __device__ __forceinline__ bool row_ckpt(const CkptOut &o, const Team<L> &t, int
 #pragma unroll
     for (int i = 0; i < V; i++) {
         byte[i] = ckpt_scale_byte(m[i], o.tf_add);
-        c[i] = e4m3_x8(v[i], __uint_as_float((254u - byte[i]) << 23) * r);
+        const float k = __uint_as_float((254u - byte[i]) << 23) * r;
+        c[i] = e4m3_x8(v[i], k);
         worst = max(worst, m[i]);
-        low |= byte[i] < 32u;
+        low |= k > kFinite;
     }
-    if (worst >= 0x7F800000u || low) {      // aside, they cost the others one comparison: a group that is not finite, and one so small that 2^-s r may overflow
+    if (worst >= 0x7F800000u || low) {      // aside, they cost the others one comparison: a group that is not finite, and one so small that 2^-s r overflows
 #pragma unroll
         for (int i = 0; i < V; i++) {
-            if (byte[i] < 32u) {
+            if (__uint_as_float((254u - byte[i]) << 23) * r > kFinite) {
                 f2 u[4];
 #pragma unroll
                 for (int j = 0; j < 4; j++) u[j] = f2_mul(v[i][j], f2_of(r, r));
