@@ -354,7 +354,9 @@ mxfp4_status_t mxfp4_change_sums_q(mxfp4_mat_t cur, mxfp4_mat_t prev, double *ou
  * by the tensor cores).  cols % 32 == 0.  A group with largest magnitude M has
  *     s = ceil(log2(M / 448))  (MXFP4_SCALE_TRUNCATION_FREE) or floor(log2 M) - 8  (MXFP4_SCALE_FLOOR),   s >= -127,
  * M = 0 taking 1e-8 (s = -35), and codes round(v 2^-s) to nearest, ties to even, magnitudes above 448 (floor scaling) to 448.
- * A group that holds Inf / NaN gets the scale byte 0xFF and codes 0 (MXFP4_DEV_NONFINITE) and reads back as NaN. */
+ * A group that holds Inf / NaN gets the scale byte 0xFF and codes 0 (MXFP4_DEV_NONFINITE) and reads back as NaN.
+ * In this and the next section, what a call writes lies apart from all else that it reads or writes unless the function says otherwise
+ * (MXFP4_INVALID_ARG; a strided matrix counts from its first byte to behind its last). */
 typedef struct {
     uint8_t *codes, *scales;   /* codes 16-byte aligned */
     int64_t rows, cols;
@@ -371,7 +373,7 @@ mxfp4_status_t mxfp4_checkpoint_load(mxfp4_ckpt_t src, void *dst, int32_t dtype,
  *     MXFP4_ACT_GEGLU, MXFP4_ACT_SWIGLU:                                              z = act(y_a) * y_b,   y = [y_a, y_b] [rows, 2 cols]
  * y, z: bf16, rows 16-byte aligned; z is computed in FP32 and rounded once.  ckpt: of y (its cols are y's); codes == NULL: none kept.
  * z == NULL: not written (the checkpoint alone).  z may lie over y (the same address and leading dimension) unless the activation is
- * gated; otherwise the outputs must not overlap y. */
+ * gated. */
 enum { MXFP4_ACT_GELU = 0, MXFP4_ACT_SILU = 1, MXFP4_ACT_GEGLU = 2, MXFP4_ACT_SWIGLU = 3 };
 mxfp4_status_t mxfp4_act_fwd(const void *y_bf16, int64_t ldy, int64_t rows, int64_t cols, int32_t act, void *z_bf16, int64_t ldz, mxfp4_ckpt_t ckpt,
                              int32_t scale_mode, uint32_t *dev_status, void *stream);

@@ -247,6 +247,9 @@ mxfp4_status_t mxfp4_checkpoint_store(const void *src, int32_t dtype, int64_t ld
     if (dst.rows == 0 || dst.cols == 0) return MXFP4_OK;
     mxfp4_status_t s;
     if ((s = check_rows(src, ld, dst.cols, dtype)) || (s = check_ckpt(dst, dst.rows, dst.cols))) return s;
+    Memory m;
+    m.written(dst.codes, dst.rows * dst.cols), m.written(dst.scales, dst.rows * dst.cols / 32), m.read(span_of_rows(src, ld, dst.rows, dst.cols, dtype_bytes(dtype)));
+    if (!m.apart()) return MXFP4_INVALID_ARG;
     const int64_t nvec = dst.cols / 8, total = dst.rows * nvec;
     const CkptOut out = {dst.codes, dst.scales, ckpt_tf_add(scale_mode)};
     unsigned blocks;
@@ -268,6 +271,9 @@ mxfp4_status_t mxfp4_checkpoint_load(mxfp4_ckpt_t src, void *dst, int32_t dtype,
     if (src.rows == 0 || src.cols == 0) return MXFP4_OK;
     mxfp4_status_t s;
     if ((s = check_rows(dst, ld, src.cols, dtype)) || (s = check_ckpt(src, src.rows, src.cols))) return s;
+    Memory m;
+    m.written(span_of_rows(dst, ld, src.rows, src.cols, dtype_bytes(dtype))), m.read(src.codes, src.rows * src.cols), m.read(src.scales, src.rows * src.cols / 32);
+    if (!m.apart()) return MXFP4_INVALID_ARG;
     const int64_t nvec = src.cols / 8, total = src.rows * nvec;
     unsigned blocks;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -292,7 +298,10 @@ mxfp4_status_t mxfp4_act_fwd(const void *y_bf16, int64_t ldy, int64_t rows, int6
     if ((s = check_rows(y_bf16, ldy, ycols, MXFP4_OUT_BF16))) return s;
     if (z_bf16 && (s = check_rows(z_bf16, ldz, cols, MXFP4_OUT_BF16))) return s;
     if (ckpt.codes && (s = check_ckpt(ckpt, rows, ycols))) return s;
-    if (z_bf16 && !over_or_apart(z_bf16, ldz, cols, y_bf16, ldy, ycols, rows)) return MXFP4_INVALID_ARG;
+    Memory m;
+    m.written(span_of_rows(z_bf16, ldz, rows, cols, 2)), m.read(span_of_rows(y_bf16, ldy, rows, ycols, 2));
+    if (ckpt.codes) m.written(ckpt.codes, rows * ycols), m.written(ckpt.scales, rows * ycols / 32);
+    if ((z_bf16 && !over_or_apart(z_bf16, ldz, cols, y_bf16, ldy, ycols, rows)) || !m.apart(z_bf16 != nullptr, 1)) return MXFP4_INVALID_ARG;
     const int64_t nvec = cols / 8, total = rows * nvec;
     const CkptOut out = {ckpt.codes, ckpt.scales, ckpt_tf_add(scale_mode)};
     unsigned blocks;
@@ -315,7 +324,9 @@ mxfp4_status_t mxfp4_act_bwd(const void *dz_bf16, int64_t lddz, mxfp4_ckpt_t ckp
     if (rows == 0 || cols == 0) return MXFP4_OK;
     mxfp4_status_t s;
     if ((s = check_rows(dz_bf16, lddz, cols, MXFP4_OUT_BF16)) || (s = check_rows(dy_bf16, lddy, ckpt.cols, MXFP4_OUT_BF16)) || (s = check_ckpt(ckpt, rows, ckpt.cols))) return s;
-    if (!over_or_apart(dy_bf16, lddy, ckpt.cols, dz_bf16, lddz, cols, rows)) return MXFP4_INVALID_ARG;
+    Memory m;
+    m.written(span_of_rows(dy_bf16, lddy, rows, ckpt.cols, 2)), m.read(ckpt.codes, rows * ckpt.cols), m.read(ckpt.scales, rows * ckpt.cols / 32);
+    if (!over_or_apart(dy_bf16, lddy, ckpt.cols, dz_bf16, lddz, cols, rows) || !m.apart()) return MXFP4_INVALID_ARG;
     const int64_t nvec = cols / 8, total = rows * nvec;
     unsigned blocks;
     if ((s = blocks_of(total, 2, &blocks))) return s;

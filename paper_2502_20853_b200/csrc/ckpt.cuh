@@ -192,6 +192,28 @@ inline bool rows_on_32(const void *p, int64_t ld) { return ((reinterpret_cast<ui
 inline int64_t dtype_bytes(int dtype) { return dtype == MXFP4_OUT_FP32 ? 4 : 2; }
 inline Span span_of_rows(const void *p, int64_t ld, int64_t rows, int64_t cols, int64_t bytes) { return span_of(p, p && rows > 0 ? bytes * ((rows - 1) * ld + cols) : 0); }
 
+// What a call writes and what it reads.  A thread reads and writes in an order of its own, so that written memory has to lie apart from all other.
+struct Memory {
+    Span w[9], r[13];
+    int writes = 0, reads = 0;
+
+    void written(const void *p, int64_t bytes) { if (p) w[writes++] = span_of(p, bytes); }
+    void written(const Span &s) { if (s.hi) w[writes++] = s; }
+    void read(const void *p, int64_t bytes) { if (p) r[reads++] = span_of(p, bytes); }
+    void read(const Span &s) { if (s.hi) r[reads++] = s; }
+    // `over`: the first so many of the written may lie over the first `under` of the read (that is the caller's to check)
+    bool apart(int over = 0, int under = 0) const
+    {
+        for (int i = 0; i < writes; i++) {
+            for (int k = 0; k < i; k++)
+                if (meet(w[i], w[k])) return false;
+            for (int k = i < over ? under : 0; k < reads; k++)
+                if (meet(w[i], r[k])) return false;
+        }
+        return true;
+    }
+};
+
 // A row-major matrix argument: a present pointer on 16 bytes, rows that do not overlap and start on 16 bytes.
 inline mxfp4_status_t check_rows(const void *p, int64_t ld, int64_t cols, int dtype)
 {

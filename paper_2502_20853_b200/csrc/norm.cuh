@@ -257,6 +257,13 @@ inline mxfp4_status_t check_side(const mxfp4_norm_t &n)
     if ((n.dtype != MXFP4_OUT_BF16 && n.dtype != MXFP4_OUT_FP32) || !(n.eps >= 0.0f)) return MXFP4_INVALID_ARG;
     return aligned16(n.weight) && aligned16(n.bias) ? MXFP4_OK : MXFP4_MISALIGNED;
 }
+// The parameters, as memory that is read.
+inline void read_plan(Memory &m, const mxfp4_residual_norm_t &n)
+{
+    for (const mxfp4_norm_t *s : {&n.pre, &n.post})
+        if (s->kind != MXFP4_NORM_NONE) m.read(s->weight, n.cols * dtype_bytes(s->dtype)), m.read(s->bias, n.cols * dtype_bytes(s->dtype));
+    m.read(span_of_rows(n.gate, n.gates > 1 ? n.ld_gate : n.cols, n.gates, n.cols, dtype_bytes(n.gate_dtype)));
+}
 inline NormSide side_of(const mxfp4_norm_t &n) { return {n.weight, n.bias, n.dtype == MXFP4_OUT_FP32, n.kind == MXFP4_NORM_RMS, n.eps}; }
 
 // What the two directions check alike.

@@ -209,19 +209,27 @@ mxfp4_status_t mxfp4_residual_norm_bwd(const mxfp4_residual_norm_t *n, const mxf
     if (reinterpret_cast<uintptr_t>(workspace) & 255u) return MXFP4_MISALIGNED;
     const bool sb = b->db_pre, sa = post && (b->db_post || (b->dgate && n->post.bias));
     const RowPlan plan = bwd_plan(rows, cols, 2 + sb + sa);
-    if (workspace_bytes < mxfp4_residual_norm_workspace_bytes(rows, cols, n->gates)) return MXFP4_WORKSPACE_TOO_SMALL;
+    const size_t needed = mxfp4_residual_norm_workspace_bytes(rows, cols, n->gates);
+    if (workspace_bytes < needed) return MXFP4_WORKSPACE_TOO_SMALL;
     {
         // dx and df are written row by row while later rows are still to be read
         const Span dx = span_of_rows(b->dx, b->lddx, rows, cols, xb), df = span_of_rows(b->df_bf16, b->lddf, rows, cols, 2);
         const Span dxo = span_of_rows(b->dx_out, b->lddxo, rows, cols, xb), dh = span_of_rows(b->dh_bf16, b->lddh, rows, cols, 2);
-        if (meet(dx, df) || !rows_over_or_apart(dx, b->lddx, xb, dxo, b->lddxo, xb) || !rows_over_or_apart(dx, b->lddx, xb, dh, b->lddh, 2) ||
+        if (!rows_over_or_apart(dx, b->lddx, xb, dxo, b->lddxo, xb) || !rows_over_or_apart(dx, b->lddx, xb, dh, b->lddh, 2) ||
             !rows_over_or_apart(df, b->lddf, 2, dxo, b->lddxo, xb) || !rows_over_or_apart(df, b->lddf, 2, dh, b->lddh, 2))
             return MXFP4_INVALID_ARG;
-        const Span kept[4] = {pre && eight ? span_of(b->x_ckpt.codes, rows * cols) : Span{0, 0}, need_f && eight ? span_of(b->f_ckpt.codes, rows * cols) : Span{0, 0},
-                              pre && !eight ? span_of_rows(b->x_out, b->ldxo, rows, cols, xb) : Span{0, 0},
-                              need_f && !eight ? span_of_rows(b->f_bf16, b->ldf, rows, cols, 2) : Span{0, 0}};
-        for (const Span &k : kept)
-            if (k.hi && (meet(dx, k) || meet(df, k))) return MXFP4_INVALID_ARG;
+        Memory m;
+        m.written(dx), m.written(df), m.read(dxo), m.read(dh);
+        const int over = m.writes, under = m.reads;
+        for (const float *g : {b->dw_pre, b->db_pre, b->dw_post, b->db_post}) m.written(g, cols * 4);
+        m.written(b->dgate, n->gates * cols * 4), m.written(workspace, (int64_t)needed);
+        if (pre && eight) m.read(b->x_ckpt.codes, rows * cols), m.read(b->x_ckpt.scales, rows * cols / 32);
+        if (need_f && eight) m.read(b->f_ckpt.codes, rows * cols), m.read(b->f_ckpt.scales, rows * cols / 32);
+        if (pre && !eight) m.read(span_of_rows(b->x_out, b->ldxo, rows, cols, xb));
+        if (need_f && !eight) m.read(span_of_rows(b->f_bf16, b->ldf, rows, cols, 2));
+        if (pre || post) m.read(b->stats, 16 * rows);
+        read_plan(m, *n);
+        if (!m.apart(over, under)) return MXFP4_INVALID_ARG;
     }
     NormBwd p = {};
     p.dh = static_cast<const __nv_bfloat16 *>(b->dh_bf16), p.dxo = b->dx_out, p.lddh = b->lddh, p.lddxo = b->lddxo, p.stats = b->stats;

@@ -41,8 +41,17 @@ mxfp4_status_t mxfp4_residual_norm_fwd(const mxfp4_residual_norm_t *n, const voi
     const Span sx = span_of_rows(x, ldx, rows, cols, xb), sf = span_of_rows(f_bf16, ldf, rows, cols, 2);
     const Span so = span_of_rows(x_out, ldxo, rows, cols, xb), sh = span_of_rows(h_bf16, ldh, rows, cols, 2);
     if (!rows_over_or_apart(so, ldxo, xb, sx, ldx, xb) || !rows_over_or_apart(so, ldxo, xb, sf, ldf, 2) || !rows_over_or_apart(sh, ldh, 2, sx, ldx, xb) ||
-        !rows_over_or_apart(sh, ldh, 2, sf, ldf, 2) || meet(so, sh))
+        !rows_over_or_apart(sh, ldh, 2, sf, ldf, 2))
         return MXFP4_INVALID_ARG;
+    Memory m;
+    m.written(so), m.written(sh), m.read(sx), m.read(sf);
+    const int over = m.writes, under = m.reads;
+    for (const mxfp4_ckpt_t *c : {&x_ckpt, &f_ckpt})
+        if (c->codes) m.written(c->codes, rows * cols), m.written(c->scales, rows * cols / 32);
+    if (hq) m.written(hq->data, rows * cols / 2), m.written(hq->scales, (int64_t)mxfp4_scale_bytes(rows, cols));
+    if (pre || post) m.written(stats, 16 * rows);
+    read_plan(m, *n);
+    if (!m.apart(over, under)) return MXFP4_INVALID_ARG;
     NormFwd p = {};
     const RowPlan plan = row_plan(cols, 0);
     p.warps = plan.warps(), p.teams = plan.teams;
