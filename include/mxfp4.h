@@ -393,7 +393,10 @@ mxfp4_status_t mxfp4_act_bwd(const void *dz_bf16, int64_t lddz, mxfp4_ckpt_t ckp
  * optional (1 and 0).  gate: g is one row of [gates, cols] for each rows / gates consecutive rows (one gate: a layer scale; one
  * per sequence: what a conditioning projection gives; NULL with gates = 0: 1).
  * Everything is computed in FP32 (statistics by two passes over the row in registers) and rounded once per output; h and the
- * checkpoints come from the unrounded x'. */
+ * checkpoints come from the unrounded x'.
+ * A row of which a sum or a sum of squares leaves FP32 (it holds Inf or NaN, or squares that add up to more than 3.4e38) has no deviation: 1 / sqrt(var + eps),
+ * the whole normalized row and what is made of it are NaN, under an RMS norm as under a layer norm, and not 0 where the deviation's
+ * infinity would make them so.  Checkpoints and quantized results of such a row raise MXFP4_DEV_NONFINITE. */
 enum { MXFP4_NORM_NONE = 0, MXFP4_NORM_LAYER = 1, MXFP4_NORM_RMS = 2 };
 typedef struct {
     int32_t kind;              /* MXFP4_NORM_* */

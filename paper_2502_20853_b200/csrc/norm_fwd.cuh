@@ -36,7 +36,7 @@ struct NormFwd {
     uint32_t *dev_status;
 };
 
-// s / n, by 1 / n and the remainder
+// s / n, by 1 / n and the remainder; NaN where s is not finite, which the header promises of such a row
 __device__ __forceinline__ float over(float s, float n, float inv)
 {
     const float q = s * inv;

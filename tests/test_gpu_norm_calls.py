@@ -51,3 +51,34 @@ def test_tiny_groups_of_tiny_rows(mx, dtype, eps):
     assert bool((far <= 0).all()), far.amax(1)
     m = want.abs().reshape(16, -1, 32).amax(2)
     assert bool((torch.ldexp(m, -(c.scales.to(torch.int32) - 127)) > 223).all())      # the scale is the group's
+
+
+@pytest.mark.parametrize("kind", ["NORM_LAYER", "NORM_RMS"])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("value", [float("inf"), float("-inf"), float("nan"), 1e25])
+@pytest.mark.parametrize("where", ["x", "f"])
+def test_rows_without_a_deviation_in_fp32(mx, kind, dtype, value, where):
+    """NaN throughout and flagged, of an RMS norm too: not zeros, which the infinite deviation would give."""
+    rows, cols, row = 40, 160, 11
+    g = torch.Generator(device="cuda").manual_seed(7)
+    rnd = lambda *s: torch.randn(*s, device="cuda", generator=g)  # noqa: E731
+    x, f = rnd(rows, cols).to(dtype), rnd(rows, cols).to(BF16)
+    (x if where == "x" else f)[row, 70] = value
+    norm = mx.Norm(getattr(mx, kind), 1 + 0.2 * rnd(cols), 0.1 * rnd(cols))
+    rest = torch.arange(rows, device="cuda") != row
+    st, hq = mx.new_status(), mx.QMat(rows, cols)
+    x_out, h, ctx = mx.residual_norm_fwd(x, f, pre=norm, post=norm, hq=hq, dev_status=st)
+    assert int(st.item()) == mx.DEV_NONFINITE
+    assert bool(torch.isnan(h[row]).all()) and bool(torch.isfinite(h[rest]).all())
+    assert bool((ctx.x.scales[row] == 255).all()) and bool((ctx.x.codes[row] == 0).all()) and bool((ctx.x.scales[rest] != 255).all())
+    assert bool(torch.isnan(ctx.stats[1, row])) and bool(torch.isfinite(ctx.stats[:, rest]).all())
+    if where == "f":
+        assert bool(torch.isnan(x_out[row]).all()) and bool(torch.isnan(ctx.stats[3, row])) and bool((ctx.f.scales[row] == 255).all())
+    else:                               # x' itself is what the sum says
+        only = torch.arange(cols, device="cuda") != 70
+        assert bool(torch.isfinite(x_out[row, only]).all()) and bool(torch.isfinite(ctx.stats[2:, row]).all()) and bool((ctx.f.scales[row] != 255).all())
+        big = float(x_out[row, 70])
+        assert big != big if value != value else big == float(x[row, 70])
+    grads = mx.residual_norm_bwd(rnd(rows, cols).to(BF16), rnd(rows, cols).to(dtype), ctx)
+    assert bool(torch.isnan(grads.dx[row]).all()) and bool(torch.isfinite(grads.dx[rest]).all())
+    assert bool(torch.isnan(grads.df[row]).all()) and bool(torch.isfinite(grads.df[rest]).all())
