@@ -111,7 +111,7 @@ class CResidualNormBwd(C.Structure):
                 ("dgate", C.c_void_p)]
 
 
-_NO_CKPT, _NO_NORM = CCkpt(None, None, 0, 0), CNorm(0, 0, None, None, 0.0, 0)
+_NO_CKPT = CCkpt(None, None, 0, 0)
 
 _lib = None
 

@@ -442,7 +442,7 @@ template <class XT, bool EIGHT> cudaError_t launch_norm_bwd(const NormBwd &p, co
         constexpr int L = decltype(l)::value, V = decltype(v)::value;
         return with_bools(need_f, post, pre, [&](auto f, auto q, auto r) -> cudaError_t {
             constexpr bool F = decltype(f)::value, Q = decltype(q)::value, R = decltype(r)::value;
-            if constexpr ((Q && !F) || (!R && !F && EIGHT)) {
+            if constexpr ((Q && !F) || (!R && !F && EIGHT) || !some_width_has(V, L, decltype(full)::value, true)) {
                 return cudaErrorInvalidValue;     // does not occur
             } else {
                 return with_bools(sb, sa, false, [&](auto b, auto a, auto) -> cudaError_t {

@@ -376,8 +376,8 @@ template <class XT> cudaError_t launch_norm_fwd(NormFwd &p, const RowPlan &plan,
         constexpr int L = decltype(l)::value, V = decltype(v)::value;
         return with_bools(has_f, post, pre, [&](auto f, auto q, auto r) -> cudaError_t {
             constexpr bool F = decltype(f)::value, Q = decltype(q)::value, R = decltype(r)::value;
-            if constexpr (!F && (Q || !R)) {
-                return cudaErrorInvalidValue;     // refused by the caller
+            if constexpr ((!F && (Q || !R)) || !some_width_has(V, L, decltype(full)::value, false)) {
+                return cudaErrorInvalidValue;     // refused by the caller, or no width's plan
             } else {
                 const size_t planes = (size_t)(p.has_cw + p.has_cb + (R && p.pre.w) + (R && p.pre.b)) * p.cols * 4;
                 // two stages in half of an SM's shared memory, or as many as there is room for in all of it (one at least: 128 KB of planes
