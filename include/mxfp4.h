@@ -428,7 +428,7 @@ mxfp4_status_t mxfp4_residual_norm_fwd(const mxfp4_residual_norm_t *n, const voi
  * Of the forward pass: stats, and x^ and f^ either as checkpoints (codes != NULL) or as x_out and f themselves (both or neither of
  * the two in 8 bits; x_out is read where there is N_pre, f where there is N_post or a gate).
  * Out, all optional but dx: dx (x_dtype), df (bf16; NULL also means that there was no f), and in FP32, written whole: dw_pre, db_pre, dw_post, db_post
- * [cols], dgate [gates, cols].  Sums over rows are taken in FP32 in an order that depends on the shape and the number of SMs alone: the same
+ * [cols], dgate [gates, cols].  Sums over rows are taken in FP32 in an order that goes by the shape and the gradients asked for alone: the same
  * call gives the same bits.  dx may lie over dx_out (the same address and leading dimension), df over dh likewise.
  * workspace: >= mxfp4_residual_norm_workspace_bytes, 256-byte aligned; its contents do not matter. */
 size_t mxfp4_residual_norm_workspace_bytes(int64_t rows, int64_t cols, int64_t gates);
