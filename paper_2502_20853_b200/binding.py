@@ -138,8 +138,8 @@ def _like(x):
 
 
 def _vectors(n, cols, device):
-    """n FP32 vectors: in one buffer up to 1 MiB, where the allocations would show."""
-    if n > 2 and n * cols <= 1 << 18 and ALLOC_HOOK is None:
+    """n FP32 vectors of a norm's columns (four of 8192 at most): from three on in one buffer, as the allocations would show."""
+    if n > 2 and ALLOC_HOOK is None:
         return _new((n, cols), torch.float32, device).unbind(0)
     return [_new((cols,), torch.float32, device) for _ in range(n)]
 
