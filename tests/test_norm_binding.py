@@ -1,5 +1,7 @@
 """The binding of the residual norms, activations and checkpoints on tensors of the CPU (the library refuses or returns before it touches them): what it
 takes and what it refuses."""
+import copy
+
 import pytest
 import torch
 
@@ -91,3 +93,35 @@ def test_what_comes_beside_the_matrices_is_on_their_device():
     for w in (_Elsewhere(work), work[::2]):
         with pytest.raises(AssertionError, match="workspace"):
             mx.residual_norm_bwd(f, x, ctx, workspace=w)
+
+
+@pytest.mark.parametrize("rows,cols", [(1, 32), (3, 96), (257, 416), (0, 64)])
+def test_checkpoint_in_one_buffer(rows, cols):
+    """Codes and scales that the binding allocates: one behind the other, the same addresses whether the views have been made or not, in copies too."""
+    for views in ("", "codes", "scales", "codes scales", "scales codes"):
+        c = mx.Checkpoint.empty(rows, cols, "cpu")
+        first = c._at((rows, cols), -1)
+        for name in views.split():
+            getattr(c, name)
+        assert c._at((rows, cols), -1) == first and c.device == torch.device("cpu") and c.shape == (rows, cols)
+        assert c.codes.shape == (rows, cols) and c.scales.shape == (rows, cols // 32) and c.codes.is_contiguous() and c.scales.is_contiguous()
+        if rows:
+            assert first == (c.codes.data_ptr(), c.scales.data_ptr()) and first[1] - first[0] == rows * cols
+            c.codes.fill_(3), c.scales.fill_(5)
+            assert bool((c._buf[:rows * cols] == 3).all()) and bool((c._buf[rows * cols:] == 5).all())
+            d = copy.deepcopy(c)
+            assert torch.equal(d.codes, c.codes) and torch.equal(d.scales, c.scales) and d._at((rows, cols), -1) == (d.codes.data_ptr(), d.scales.data_ptr())
+            c.codes.zero_()
+            assert bool((d.codes == 3).all())
+        with pytest.raises(AssertionError):
+            c._at((rows + 1, cols), -1)
+        with pytest.raises(AssertionError):
+            c._at((rows, cols), 0)
+
+
+def test_gradients_in_one_buffer():
+    for n in range(5):
+        v = list(binding._vectors(n, 96, "cpu"))
+        assert len(v) == n and all(t.shape == (96,) and t.dtype == F32 and t.is_contiguous() and t.data_ptr() % 16 == 0 for t in v)
+        spans = sorted((t.data_ptr(), t.data_ptr() + 4 * 96) for t in v)
+        assert all(a[1] <= b[0] for a, b in zip(spans, spans[1:]))
